@@ -1,0 +1,538 @@
+"""The operators around the retrieval index, as cases that can be timed.
+
+What a server runs beside the index: rotary positions, the block tables of a
+paged cache, writing keys and values to it in 8 bits, attention over it (every
+key, or the keys that the index lists), and causal attention over the prompts.
+Head counts are those of ``workloads`` (LLaMA-3.1-8B-shaped 32 / 8 and
+Qwen2.5-7B-shaped 28 / 4 layers); lengths run from single tokens to the long
+caches of its decode workloads.
+
+With ``own`` false ``run`` computes the operators in elementary torch
+operations; with ``own`` true it calls the library.
+
+The cache: blocks of 64 tokens; per (block, KV head) keys [64, d] and values
+[d, 64] as E4M3 values, and one power-of-two scale for each of the two.
+
+Kinds of case ("do"): rope, tables, write, attend (listed or not), prompt.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+D = 128       # head dimension of every configuration
+BLOCK = 64    # tokens per cache block
+THETA = 500000.0
+DEV = "cuda"
+F8 = torch.float8_e4m3fn
+_DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+_ES = {"f32": 4, "bf16": 2}
+
+
+# ---------------------------------------------------------------- the cases
+
+def listed():
+    return [
+        # the new tokens of one decode step of 64 conversations
+        dict(name="rope_step", do="rope", T=64, H_q=32, H_kv=8, dt="bf16", axes=1, inverse=False, far=131072),
+        # a video prompt's three axes in the training direction (the gradient's rotation), float32
+        dict(name="rope_video_f32_inverse", do="rope", T=16384, H_q=28, H_kv=4, dt="f32", axes=3, inverse=True,
+             far=16384),
+        # block tables of one decode step: one new token each, most blocks there already
+        dict(name="tables_step", do="tables", B=64, ctx=131072, new=1, mix=1),
+        # block tables of a large batch of new and continued prompts
+        dict(name="tables_prompts", do="tables", B=512, ctx=4096, new=512, mix=2),
+        # one decode step's keys and values, each into its own partly filled block
+        dict(name="write_step", do="write", B=64, ctx=8192, new=1, H_kv=8, dt="bf16", mix=3),
+        # the keys and values of whole prompts, float32, ragged
+        dict(name="write_prompts_f32", do="write", B=24, ctx=300, new=2600, H_kv=4, dt="f32", mix=4),
+        # a short conversation's decode step: latency counts
+        dict(name="attend_step_4k", do="attend", B=1, H_q=32, H_kv=8, Q=1, N=4001, k=0, dt="bf16", mix=5),
+        # decode of a long ragged batch, float32 queries
+        dict(name="attend_batch_131k", do="attend", B=8, H_q=28, H_kv=4, Q=1, N=131072, k=0, dt="f32", mix=6),
+        # the index's lists read from a long cache, a batch of decode steps
+        dict(name="attend_lists_131k", do="attend", B=8, H_q=32, H_kv=8, Q=1, N=131072, k=64, dt="f32", mix=7),
+        # a few short questions arriving together
+        dict(name="prompt_short", do="prompt", B=5, H_q=32, H_kv=8, N=333, dt="bf16", mix=8),
+        # one prompt of the paper's length in float32
+        dict(name="prompt_4k_f32", do="prompt", B=1, H_q=28, H_kv=4, N=4096, dt="f32", mix=9),
+        # packed long prompts
+        dict(name="prompt_packed_8k", do="prompt", B=3, H_q=32, H_kv=8, N=8192, dt="bf16", mix=10),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    H_q, H_kv = rng.choice([(32, 8), (28, 4), (8, 8), (16, 2), (12, 1), (5, 5)])
+    dt = rng.choice(["bf16", "f32"])
+    mix = rng.randrange(1 << 30)
+    do = rng.choice(["rope", "tables", "write", "attend", "lists", "prompt"])
+    if do == "rope":
+        return dict(do=do, T=_log_int(rng, 1, 16384), H_q=H_q, H_kv=H_kv, dt=dt, axes=rng.choice([1, 2, 3]),
+                    inverse=rng.random() < 0.4, far=_log_int(rng, 100, 1 << 20))
+    if do == "tables":
+        return dict(do=do, B=_log_int(rng, 1, 2000), ctx=_log_int(rng, 1, 131072), new=_log_int(rng, 1, 128), mix=mix)
+    if do == "write":
+        return dict(do=do, B=_log_int(rng, 1, 64), ctx=_log_int(rng, 1, 8192), new=_log_int(rng, 1, 900), H_kv=H_kv,
+                    dt=dt, mix=mix)
+    if do == "prompt":
+        B = rng.choice([1, 2, 3, 5, 8])
+        return dict(do=do, B=B, H_q=H_q, H_kv=H_kv, N=_log_int(rng, 1, 8192 // (1 if B == 1 else B)), dt=dt, mix=mix)
+    B = _log_int(rng, 1, 32)
+    return dict(do="attend", B=B, H_q=H_q, H_kv=H_kv, Q=rng.choice([1, 1, 1, 2, 4]), N=_log_int(rng, 1, 131072 // B),
+                k=rng.choice([64, 64, 17]) if do == "lists" else 0, dt=dt, mix=mix)
+
+
+# The lengths belong to the case, not to its inputs: one of the batch has the
+# full length, the others any from a quarter of it (prompts), or any at all.
+
+def _lengths(mix, B, most, least):
+    rng = random.Random(mix)
+    n = [rng.randint(min(least, most), most) for _ in range(B)]
+    n[rng.randrange(B)] = most
+    return n
+
+
+def _ctx_new(c):
+    ctx = _lengths(c["mix"], c["B"], c["ctx"], 0)
+    new = _lengths(c["mix"] + 1, c["B"], c["new"], 1 if c["new"] == 1 else 0)
+    return ctx, new
+
+
+def _blocks(n):
+    return -(-n // BLOCK)
+
+
+def _sections(axes):
+    return {1: (64,), 2: (32, 32), 3: (16, 24, 24)}[axes]
+
+
+def _lens(c):
+    return _lengths(c["mix"], c["B"], c["N"], max(1, c["N"] // 4))
+
+
+# ---------------------------------------------------------------- inputs
+
+def _gen(seed):
+    g = torch.Generator(DEV)
+    g.manual_seed(int(seed) * 2654435761 % (1 << 31) + 17)
+    return g
+
+
+def _int(values, dev=DEV):
+    return torch.tensor(values, dtype=torch.int32, device=dev)
+
+
+def _randn(g, *shape):
+    return torch.randn(shape, generator=g, device=DEV)
+
+
+def _outlier(g, H):
+    """Per-channel size of a head's keys: a few channels are far larger."""
+    s = torch.ones(H, D, device=DEV)
+    at = torch.randint(0, D, (H, 4), generator=g, device=DEV)
+    return s.scatter_(1, at, 4.0)
+
+
+def _free_list(g, n_blocks):
+    return torch.randperm(n_blocks, generator=g, device=DEV).to(torch.int32)
+
+
+def _held_tables(order, ctx, max_blocks):
+    """Tables of blocks for `ctx` tokens a request, taken in order; what no
+    request holds yet is -1.  Returns them and the blocks that are left."""
+    held = [_blocks(n) for n in ctx]
+    tables = torch.full((len(ctx), max_blocks), -1, dtype=torch.int32, device=DEV)
+    at = 0
+    for b, h in enumerate(held):
+        tables[b, :h] = order[at:at + h]
+        at += h
+    return tables, order[at:].clone()
+
+
+def _filled_cache(g, n_blocks, H_kv):
+    """A cache as earlier writes leave it: values of size 1 with larger key
+    channels, the scale of most blocks 2^-5 (keys) and 2^-6 (values)."""
+    size = _outlier(g, H_kv)[None, :, None, :]
+    up = torch.randint(0, 3, (n_blocks, H_kv, 2), generator=g, device=DEV).float()
+    scales = torch.exp2(up - torch.tensor([5.0, 6.0], device=DEV)).contiguous()
+    k = torch.empty(n_blocks, H_kv, BLOCK, D, dtype=F8, device=DEV)
+    v = torch.empty(n_blocks, H_kv, D, BLOCK, dtype=F8, device=DEV)
+    for at in range(0, n_blocks, 1024):
+        n = min(1024, n_blocks - at)
+        s = scales[at:at + n]
+        x = _randn(g, n, H_kv, BLOCK, D) * (size / s[:, :, 0, None, None])
+        k[at:at + n] = x.clamp_(-448, 448).to(F8)
+        x = _randn(g, n, H_kv, D, BLOCK) / s[:, :, 1, None, None]
+        v[at:at + n] = x.clamp_(-448, 448).to(F8)
+    return k, v, scales
+
+
+def prepare(case, seed):
+    c, g = case, _gen(seed)
+    dt = _DT.get(c.get("dt"))
+    s = {"case": c}
+    if c["do"] == "rope":
+        s["q"] = _randn(g, c["T"], c["H_q"], D).to(dt)
+        s["k"] = (_randn(g, c["T"], c["H_kv"], D) * _outlier(g, c["H_kv"])).to(dt)
+        s["pos"] = torch.randint(0, c["far"], (c["axes"], c["T"]), generator=g, device=DEV).to(torch.int32)
+        s["q_out"], s["k_out"] = torch.empty_like(s["q"]), torch.empty_like(s["k"])
+    elif c["do"] in ("tables", "write"):
+        ctx, new = _ctx_new(c)
+        T, B = sum(new), c["B"]
+        max_blocks = _blocks(c["ctx"] + c["new"])
+        n_blocks = sum(_blocks(a + b) for a, b in zip(ctx, new)) + 16
+        tables, free = _held_tables(_free_list(g, n_blocks), ctx, max_blocks)
+        s.update(ctx=_int(ctx), new=_int(new), free=free, tables=tables, T=T,
+                 slots=torch.full((T,), -1, dtype=torch.int32, device=DEV),
+                 pos=torch.zeros(T, dtype=torch.int32, device=DEV),
+                 cu=torch.zeros(B + 1, dtype=torch.int32, device=DEV),
+                 lens=torch.zeros(B, dtype=torch.int32, device=DEV),
+                 counts=torch.zeros(2, dtype=torch.int32, device=DEV))
+        if c["do"] == "write":
+            _plain_tables(s)  # the slots, as the step before gives them
+            H = c["H_kv"]
+            s["k_cache"], s["v_cache"], s["scales"] = _filled_cache(g, n_blocks, H)
+            s["k"] = (_randn(g, T, H, D) * _outlier(g, H)).to(dt)
+            s["v"] = (_randn(g, T, H, D) * torch.exp(0.5 * _randn(g, T, H, 1))).to(dt)
+    elif c["do"] == "attend":
+        lens, B, Q = _lens(c), c["B"], c["Q"]
+        n_blocks = sum(_blocks(n) for n in lens) + 3
+        s["tables"], _ = _held_tables(_free_list(g, n_blocks), lens, _blocks(c["N"]))
+        s["lens"] = _int(lens)
+        s["k_cache"], s["v_cache"], s["scales"] = _filled_cache(g, n_blocks, c["H_kv"])
+        s["q"] = (1.5 * _randn(g, B, c["H_q"], Q, D)).to(dt)
+        s["out"] = torch.empty_like(s["q"])
+        if c["k"]:
+            # the lists that the index returns: distinct keys, -1 behind a short row's
+            u = torch.rand(B, c["H_q"], Q, c["k"], generator=g, device=DEV, dtype=torch.float64)
+            n = s["lens"].double()[:, None, None, None] - Q + 1
+            step = n / c["k"]  # one key of each k-th part of the row
+            j = ((torch.arange(c["k"], device=DEV) + u) * step).floor()
+            back = torch.cat([torch.full_like(j[..., :1], -1), j[..., :-1]], -1)
+            s["top_idx"] = torch.where((j > back) & (j < n), j, -1.0).to(torch.int32)
+    else:
+        lens, H, Hk = _lens(c), c["H_q"], c["H_kv"]
+        T = sum(lens)
+        s["cu"] = _int([sum(lens[:i]) for i in range(len(lens) + 1)])
+        s["q"] = (1.5 * _randn(g, T, H, D)).to(dt)
+        s["k"] = (_randn(g, T, Hk, D) * _outlier(g, Hk)).to(dt)
+        s["v"] = _randn(g, T, Hk, D).to(dt)
+        s["out"] = torch.empty_like(s["q"])
+    return s
+
+
+# ---------------------------------------------------------------- plain forms
+
+def _plain_rope(s):
+    c = s["case"]
+    m = torch.arange(D // 2, device=DEV, dtype=torch.float64)
+    axis = torch.repeat_interleave(torch.arange(c["axes"], device=DEV),
+                                   torch.tensor(_sections(c["axes"]), device=DEV), output_size=D // 2)
+    # far positions: the angle in 64 bits
+    a = s["pos"][axis].double().T * torch.pow(THETA, -2.0 * m / D)
+    cos, sin = a.cos().float()[:, None, :], a.sin().float()[:, None, :]
+    if c["inverse"]:
+        sin = -sin
+    out = []
+    for x in (s["q"], s["k"]):
+        x1, x2 = x[..., :D // 2].float(), x[..., D // 2:].float()
+        out.append(torch.cat([x1 * cos - x2 * sin, x1 * sin + x2 * cos], -1).to(x.dtype))
+    return out
+
+
+def _plain_tables(s):
+    """New blocks in the order of the requests, then a slot for every token."""
+    ctx, new, tables, free = (s[n] for n in ("ctx", "new", "tables", "free"))
+    B, max_blocks = tables.shape
+    ctx = ctx.clamp(0, max_blocks * BLOCK).long()
+    new = new.clamp(min=0).long()
+    held, need = (ctx + BLOCK - 1) // BLOCK, (ctx + new + BLOCK - 1) // BLOCK
+    want = (need.clamp(max=max_blocks) - held).clamp(min=0)
+    base = want.cumsum(0) - want
+    got = torch.minimum((free.numel() - base).clamp(min=0), want)
+    col = torch.arange(max_blocks, device=tables.device)
+    i = col - held[:, None]
+    fresh = free[(base[:, None] + i).clamp(0, free.numel() - 1)]
+    s["tables"].copy_(torch.where((i >= 0) & (i < got[:, None]), fresh, tables))
+    lens = torch.minimum(ctx + new, (held + got) * BLOCK)
+    cu = new.cumsum(0)
+    s["lens"].copy_(lens)
+    s["cu"][1:].copy_(cu)
+    t = torch.arange(s["T"], device=tables.device)
+    b = torch.searchsorted(cu, t, right=True).clamp(max=B - 1)
+    p = ctx[b] + t - (cu - new)[b]
+    block = s["tables"][b, (p // BLOCK).clamp(max=max_blocks - 1)].long()
+    s["slots"].copy_(torch.where(p < lens[b], block * BLOCK + p % BLOCK, -1))
+    s["pos"].copy_(p)
+    s["counts"].copy_(torch.stack([got.sum(), (need - held).sum() - got.sum()]))
+    return [s[n] for n in ("tables", "slots", "pos", "cu", "lens", "counts")]
+
+
+def _scale_of(top):
+    """The least power of two s with |x| <= 448 s for all |x| <= top."""
+    m, e = torch.frexp(top)
+    e = torch.where(m > 0.875, e - 8, e - 9)
+    return torch.exp2(torch.where(top > 0, e, -100).clamp(-100, 100).float())
+
+
+def _plain_write(s):
+    slots = s["slots"].long()
+    block, off = slots // BLOCK, slots % BLOCK
+    new_run = torch.cat([block.new_ones(1, dtype=torch.bool), block[1:] != block[:-1]])
+    run = new_run.cumsum(0) - 1
+    lead = new_run.nonzero()[:, 0]   # the first token of each block
+    blk, first = block[lead], off[lead]
+    n, H = lead.numel(), s["scales"].shape[1]
+    kept = (torch.arange(BLOCK, device=DEV) < first[:, None])[:, None, :, None]   # tokens there before
+
+    def one(x, cache, which, across):
+        x = x.float()
+        top = torch.zeros(n, H, device=DEV).index_reduce_(0, run, x.abs().amax(-1), "amax")
+        old = s["scales"][blk, :, which]
+        new = torch.maximum(_scale_of(top), torch.where(first[:, None] > 0, old, 0.0))
+        was = cache.view(torch.uint8)[blk].view(F8)
+        moved = (was.float() * (old / new)[:, :, None, None]).to(F8)
+        now = torch.where(kept.transpose(2, 3) if across else kept, moved.float(), was.float())
+        y = (x / new[run][:, :, None]).to(F8).float()
+        if across:
+            now.permute(0, 3, 1, 2)[run, off] = y
+        else:
+            now.permute(0, 2, 1, 3)[run, off] = y
+        cache.view(torch.uint8)[blk] = now.to(F8).view(torch.uint8)
+        s["scales"][blk, :, which] = new
+
+    one(s["k"], s["k_cache"], 0, False)
+    one(s["v"], s["v_cache"], 1, True)
+    return [s["k_cache"], s["v_cache"], s["scales"]]
+
+
+def _softmax_rows(sc, seen):
+    """Softmax over the last axis of what is seen; rows that see nothing: 0."""
+    sc = torch.where(seen, sc, -math.inf)
+    top = sc.amax(-1, keepdim=True)
+    p = torch.exp(sc - torch.where(top > -math.inf, top, 0.0))
+    return p / p.sum(-1, keepdim=True).clamp(min=1e-37)
+
+
+def _plain_attend(s):
+    c, q = s["case"], s["q"].float()
+    B, H, Q, _ = q.shape
+    Hk = c["H_kv"]
+    G = H // Hk
+    k8, v8 = s["k_cache"].view(torch.uint8), s["v_cache"].view(torch.uint8)
+    row = s["lens"].long()[:, None] - Q + torch.arange(Q, device=DEV)    # a query's position
+    if c["k"]:
+        j = s["top_idx"].long()
+        seen = (j >= 0) & (j <= row[:, None, :, None])
+        at = j.clamp(min=0)
+        b = torch.arange(B, device=DEV)[:, None, None, None]
+        h = (torch.arange(H, device=DEV) // G)[None, :, None, None]
+        blk = s["tables"][b, at // BLOCK].long().clamp(min=0)
+        K = k8[blk, h, at % BLOCK].view(F8).float() * s["scales"][blk, h, 0][..., None]
+        V = v8[blk, h, :, at % BLOCK].view(F8).float() * s["scales"][blk, h, 1][..., None]
+        p = _softmax_rows((q[..., None, :] * K).sum(-1) / math.sqrt(D), seen)
+        return (p[..., None] * torch.where(seen[..., None], V, 0.0)).sum(-2).to(s["q"].dtype)
+    tab = s["tables"].long().clamp(min=0)
+    N = tab.shape[1] * BLOCK
+    K = (k8[tab].view(F8).float() * s["scales"][tab][..., 0, None, None]).permute(0, 2, 1, 3, 4).reshape(B, Hk, N, D)
+    V = (v8[tab].view(F8).float() * s["scales"][tab][..., 1, None, None]).permute(0, 2, 1, 4, 3).reshape(B, Hk, N, D)
+    j = torch.arange(N, device=DEV)
+    V = torch.where((j < s["lens"][:, None])[:, None, :, None], V, 0.0)
+    seen = (j <= row[..., None])[:, None, None]
+    sc = torch.matmul(q.reshape(B, Hk, G * Q, D), K.transpose(2, 3).contiguous()) / math.sqrt(D)
+    p = _softmax_rows(sc.view(B, Hk, G, Q, N), seen)
+    return torch.matmul(p.view(B, Hk, G * Q, N), V).view(B, H, Q, D).to(s["q"].dtype)
+
+
+def _plain_prompt(s):
+    """The packed prompts as a padded batch with a causal mask."""
+    c, cu, q = s["case"], s["cu"].long(), s["q"]
+    T, H, _ = q.shape
+    Hk, B, N = c["H_kv"], c["B"], c["N"]
+    i = torch.arange(N, device=DEV)
+    n = (cu[1:] - cu[:-1])[:, None]
+    at = torch.where(i < n, cu[:-1, None] + i, 0)
+    pad = lambda x: x.float()[at].transpose(1, 2).contiguous()  # noqa: E731  [B, heads, N, d]
+    qp, kp, vp = pad(q), pad(s["k"]), pad(s["v"])
+    sc = torch.matmul(qp.view(B, Hk, (H // Hk) * N, D), kp.transpose(2, 3).contiguous()) / math.sqrt(D)
+    p = _softmax_rows(sc.view(B, H, N, N), i[None, :] <= i[:, None])
+    o = torch.matmul(p.view(B, Hk, (H // Hk) * N, N), vp).view(B, H, N, D)
+    t = torch.arange(T, device=DEV)
+    b = torch.searchsorted(cu[1:], t, right=True)
+    return o[b, :, t - cu[b]].to(q.dtype)
+
+
+# ---------------------------------------------------------------- one pass
+
+def run(s):
+    do = s["case"]["do"]
+    if own:
+        from paper_2608_03228_amd import saki as S
+        if do == "rope":
+            return S.saki_rope(s["q"], s["k"], s["pos"], sections=_sections(s["case"]["axes"]), rope_theta=THETA,
+                               inverse=s["case"]["inverse"], q_out=s["q_out"], k_out=s["k_out"])
+        if do == "tables":
+            return S.saki_block_tables(s["ctx"], s["new"], s["free"], s["tables"], s["slots"], s["pos"], cu=s["cu"],
+                                       lens=s["lens"], counts=s["counts"])
+        if do == "write":
+            return S.saki_cache_write(s["k"], s["v"], s["slots"], s["k_cache"], s["v_cache"], s["scales"])
+        if do == "attend":
+            return S.saki_cache_attend(s["q"], s["k_cache"], s["v_cache"], s["scales"], s["tables"], s["lens"],
+                                       top_idx=s.get("top_idx"), out=s["out"])
+        return S.saki_attend_prompt(s["q"], s["k"], s["v"], s["cu"], out=s["out"])
+    if do == "rope":
+        return _plain_rope(s)
+    if do == "tables":
+        return _plain_tables(s)
+    if do == "write":
+        return _plain_write(s)
+    return _plain_attend(s) if do == "attend" else _plain_prompt(s)
+
+
+def work(case):
+    """Each input read once, each output written once, and the products that
+    the definition needs (two operations per multiply-add)."""
+    c = case
+    es = _ES.get(c.get("dt"), 4)
+    if c["do"] == "rope":
+        n = c["T"] * (c["H_q"] + c["H_kv"]) * D
+        return {"bytes": 2 * n * es + 4 * c["axes"] * c["T"], "flops": 3 * n}
+    if c["do"] == "tables":
+        ctx, new = _ctx_new(c)
+        fresh = sum(_blocks(a + b) - _blocks(a) for a, b in zip(ctx, new))
+        # a held block's entry is read where a new token goes into it
+        part = sum(1 for a, b in zip(ctx, new) if b and a % BLOCK)
+        return {"bytes": 4 * (2 * c["B"] + 2 * fresh + part + 2 * sum(new) + 2 * c["B"] + 3), "flops": 4 * sum(new)}
+    if c["do"] == "write":
+        ctx, new = _ctx_new(c)
+        n = sum(new) * c["H_kv"] * D
+        touched = sum(_blocks(a + b) - a // BLOCK for a, b in zip(ctx, new) if b)
+        return {"bytes": 2 * n * (es + 1) + 4 * sum(new) + 16 * touched * c["H_kv"], "flops": 4 * n}
+    if c["do"] == "attend":
+        lens, rows = _lens(c), c["B"] * c["H_q"] * c["Q"]
+        io = 2 * rows * D * es
+        if c["k"]:
+            pairs = sum(min(c["k"], n) for n in lens) * c["H_q"] * c["Q"]
+            return {"bytes": io + pairs * (2 * D + 4), "flops": 4 * D * pairs}
+        keys = sum(lens) * c["H_kv"]
+        blocks = sum(_blocks(n) for n in lens)
+        return {"bytes": io + 2 * D * keys + blocks * (4 + 8 * c["H_kv"]), "flops": 4 * D * sum(lens) * c["H_q"] * c["Q"]}
+    lens = _lens(c)
+    return {"bytes": sum(lens) * (2 * c["H_q"] + 2 * c["H_kv"]) * D * es,
+            "flops": 4 * D * c["H_q"] * sum(n * (n + 1) // 2 for n in lens)}
+
+
+# ---------------------------------------------------------------- definitions in 64 bits
+
+def _exact_rope(s):
+    c = s["case"]
+    start = [sum(_sections(c["axes"])[:i]) for i in range(c["axes"])]
+    out = []
+    for x in (s["q"], s["k"]):
+        z = torch.complex(x[..., :D // 2].double(), x[..., D // 2:].double())
+        for a, width in enumerate(_sections(c["axes"])):
+            for m in range(start[a], start[a] + width):
+                angle = s["pos"][a].double() * THETA ** (-2.0 * m / D)
+                turn = torch.polar(torch.ones_like(angle), -angle if c["inverse"] else angle)
+                z[..., m] *= turn[:, None]
+        out.append(torch.cat([z.real, z.imag], -1))
+    return out
+
+
+def _exact_write(s):
+    """Run by run on the host's view of the slots."""
+    slots = s["slots"].tolist()
+    scales = s["scales"].double()
+    caches = [s["k_cache"].double(), s["v_cache"].double().transpose(2, 3).contiguous()]
+    at = 0
+    while at < len(slots):
+        blk, first = divmod(slots[at], BLOCK)
+        n = 1
+        while at + n < len(slots) and slots[at + n] // BLOCK == blk:
+            n += 1
+        for which, x in enumerate((s["k"], s["v"])):
+            x = x[at:at + n].double()
+            top = x.abs().amax((0, 2))
+            # 448 s >= top, s a power of two: log2 is checked from both sides
+            e = torch.ceil(torch.log2(top / 448.0))
+            e = torch.where(448.0 * torch.exp2(e) < top, e + 1, e)
+            e = torch.where(448.0 * torch.exp2(e - 1) >= top, e - 1, e)
+            new = torch.exp2(e)
+            old = scales[blk, :, which].clone()
+            if first:
+                new = torch.maximum(new, old)
+                caches[which][blk, :, :first] = _round_e4m3(caches[which][blk, :, :first]
+                                                            * (old / new)[:, None, None])
+            caches[which][blk, :, first:first + n] = _round_e4m3(x.transpose(0, 1) / new[:, None, None])
+            scales[blk, :, which] = new
+        at += n
+    return [caches[0], caches[1].transpose(2, 3).contiguous(), scales]
+
+
+def _round_e4m3(x):
+    """The nearest multiple of the spacing of x's binade (at least 2^-9)."""
+    e = torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -6)))
+    step = torch.exp2(e - 3)
+    return torch.round(x / step) * step
+
+
+def _exact_attend(s):
+    c = s["case"]
+    q = s["q"].double()
+    B, H, Q, _ = q.shape
+    G = H // c["H_kv"]
+    out = torch.zeros(B, H, Q, D, dtype=torch.float64, device=DEV)
+    tables, lens = s["tables"].tolist(), s["lens"].tolist()
+    for b in range(B):
+        n = lens[b]
+        blocks = torch.tensor(tables[b][:_blocks(n)], device=DEV)
+        for g in range(c["H_kv"]):
+            sc = s["scales"][blocks, g].double()
+            K = (s["k_cache"][:, g].contiguous().view(torch.uint8)[blocks].view(F8).double()
+                 * sc[:, 0, None, None]).reshape(-1, D)[:n]
+            V = (s["v_cache"][:, g].contiguous().view(torch.uint8)[blocks].view(F8).double()
+                 * sc[:, 1, None, None]).transpose(1, 2).reshape(-1, D)[:n]
+            for h in range(g * G, (g + 1) * G):
+                for i in range(Q):
+                    end = n - Q + i + 1
+                    if end < 1:
+                        continue
+                    pick = slice(0, end)
+                    if c["k"]:
+                        pick = s["top_idx"][b, h, i].long()
+                        pick = pick[(pick >= 0) & (pick < end)]
+                        if not pick.numel():
+                            continue
+                    p = torch.softmax(K[pick] @ q[b, h, i] / math.sqrt(D), 0)
+                    out[b, h, i] = p @ V[pick]
+    return out
+
+
+def _exact_prompt(s):
+    c, cu = s["case"], s["cu"].tolist()
+    q, k, v = s["q"].double(), s["k"].double(), s["v"].double()
+    out = torch.zeros_like(q)
+    G = c["H_q"] // c["H_kv"]
+    for a, b in zip(cu[:-1], cu[1:]):
+        later = torch.ones(b - a, b - a, dtype=torch.bool, device=DEV).triu_(1)
+        for h in range(c["H_q"]):
+            sc = q[a:b, h] @ k[a:b, h // G].T
+            sc.mul_(1 / math.sqrt(D)).masked_fill_(later, -math.inf)
+            out[a:b, h] = torch.softmax(sc, -1) @ v[a:b, h // G]
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["do"] == "tables":
+        return None   # whole numbers
+    return {"rope": _exact_rope, "write": _exact_write, "attend": _exact_attend,
+            "prompt": _exact_prompt}[case["do"]](s)
