@@ -333,6 +333,126 @@ int saki_attend(const void* keys, int key_dtype, const float* values, const void
                 const float* B_q, const float* mu, const int* top_idx, int k,
                 float rope_theta, float* out, void* stream);
 
+/*
+ * Serving around the index.  The entry points below run a model's other work
+ * on the keys and values that the index stands beside: rotary positions, the
+ * block tables of a paged cache, writing that cache in 8 bits, attention over
+ * it (every key, or the lists of saki_score_topk), and attention of whole
+ * prompts.  Unlike saki_attend they take queries and keys as they are to be
+ * multiplied: a caller that wants rotary positions passes what saki_rope
+ * returns, so that a key is rotated once and not at each of its reads.
+ *
+ *   - d is 128.  Queries, keys, values and outputs are float32 or bf16
+ *     (`dtype`, the same for all of a call), rounded to nearest even where they
+ *     are written; scores, softmax, sums and scales are float32.
+ *   - Token rows [T, H, d] may lie ld elements apart (ld >= H * d, dense heads
+ *     within a row: slices of a fused projection).  Such pointers, queries and
+ *     outputs are 16-byte aligned, and ld * (size of an element) is a multiple
+ *     of 16: SAKI_ERR_ARG otherwise.
+ *   - The cache is n_blocks blocks of SAKI_CACHE_BLOCK tokens, each block
+ *     [H_kv, SAKI_CACHE_BLOCK, d] E4M3 codes for keys and the same for values,
+ *     and scales float [n_blocks, H_kv, 2] (keys, values): an element is its
+ *     code times the scale of its block and head.  H_kv * n_blocks < 2^25.
+ *   - Lengths, tables and slots are read on the device.  Table entries, slots
+ *     and list entries out of range are skipped, never followed.
+ */
+enum {
+  SAKI_CACHE_BLOCK = 64, /* tokens per cache block */
+  SAKI_CACHE_MAX_Q = 16  /* queries per request and head in saki_cache_attend */
+};
+
+/*
+ * saki_rope (GPU) -- rotary positions with one to three axes (say time, height
+ * and width).  Pair m of a head, (x_m, x_{m+d/2}), m < d/2, belongs to the axis
+ * whose section holds it (the first sections[0] pairs to axis 0, and so on) and
+ * is turned by pos[axis][t] * rope_theta^(-2m/d); with one axis this is the
+ * rotation of saki_attend.  Angles are reduced in float64.  `inverse` turns
+ * back: the inverse of the rotation, and its gradient.
+ *
+ *   q         device [T, H_q, d] rows ld_q apart (NULL with H_q = 0)
+ *   k         device [T, H_kv, d] rows ld_k apart (NULL with H_kv = 0)
+ *   pos       device int [axes, T];  sections  host int [axes], sum d/2
+ *   q_out, k_out  rows ld_q_out, ld_k_out apart; each may be its input (with
+ *             its ld), and overlaps no other array otherwise
+ * T <= 2^26.
+ */
+int saki_rope(const void* q, const void* k, int dtype, int T, int H_q, int H_kv, int d,
+              size_t ld_q, size_t ld_k, const int* pos, int axes, const int* sections,
+              float rope_theta, int inverse, void* q_out, void* k_out, size_t ld_q_out,
+              size_t ld_k_out, void* stream);
+
+/*
+ * saki_block_tables (GPU) -- block tables, slots, positions and offsets of a
+ * step, from the requests' lengths.  Request b holds ctx_lens[b] tokens in
+ * ceil(ctx_lens[b] / 64) blocks, the first entries of its row of `tables`, and
+ * gets new_lens[b] more (lengths below 0 count as 0, contexts above the row's
+ * room as that room).  The blocks that it lacks are taken from free_blocks, in
+ * order, request by request; a request gets what is left when the list ends,
+ * and a row holds max_blocks.
+ *
+ *   free_blocks  device int [n_free], entries below 2^25
+ *   tables     device int [B, max_blocks], in place: only new entries are written
+ *   slots      device int [T] out: block * 64 + offset of every new token, the
+ *              requests' tokens one after another; -1 for a token without a block
+ *   pos        device int [T] out: the token's position in its request
+ *   cu         device int [B + 1] out: a request's tokens are [cu[b], cu[b+1])
+ *   lens       device int [B] out: tokens that have a block, ctx and new
+ *   counts     device int [2] out: blocks taken (the first of the list), blocks lacking
+ * Of more than T tokens only the first T have slots and pos; with fewer, the
+ * rest of the two arrays is left as it was.
+ */
+int saki_block_tables(const int* ctx_lens, const int* new_lens, int B, const int* free_blocks,
+                      int n_free, int* tables, int max_blocks, int* slots, int* pos, int T,
+                      int* cu, int* lens, int* counts, void* stream);
+
+/*
+ * saki_cache_write (GPU) -- keys and values of T tokens to their slots, as the
+ * nearest E4M3 codes (ties to the even code) under their block's scale: the
+ * least power of two s, at least 2^-100, with |x| <= 448 s for the block's new
+ * tokens.  Where the block holds tokens before them (slots below the first new
+ * one) it is no less than the scale that is there, and if it grows, their codes
+ * are rounded to it: powers of two keep them but where they become subnormal.
+ *
+ *   k, v     device [T, H_kv, d], rows ld_k, ld_v apart; finite
+ *   slots    device int [T]; a block's tokens stand together and ascend (as
+ *            saki_block_tables gives them; else what the block then holds is
+ *            not specified); tokens with slots out of range are skipped, and
+ *            what they hold has no effect
+ *   k_cache, v_cache  device [n_blocks, H_kv, 64, d] bytes;  scales device float
+ * Codes of other slots of the blocks, and other blocks, are left as they were.
+ * T <= 2^26.
+ */
+int saki_cache_write(const void* k, const void* v, int dtype, int T, int H_kv, int d,
+                     size_t ld_k, size_t ld_v, const int* slots, void* k_cache, void* v_cache,
+                     float* scales, int n_blocks, void* stream);
+
+/* Workspace for saki_cache_attend (bytes; 0 on bad arguments): the parts of the
+ * requests that several work-groups share, at most 8.6 MB.  With lists (k > 0)
+ * the call needs none. */
+size_t saki_cache_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int max_blocks, int k);
+
+/*
+ * saki_cache_attend (GPU) -- attention of Q queries per request and head over
+ * the 8-bit cache: s_j = q_i . key_j / sqrt(d), p = softmax(s), out_i = sum_j
+ * p_j value_j.  Query i of request b stands at position lens[b] - Q + i (the
+ * newest tokens; a decode step has Q = 1) and sees the keys up to there.  With
+ * top_idx it attends only over the listed ones of them (entries that are
+ * negative, or not seen, are skipped; one listed twice counts twice).  A row
+ * without a key writes zeros.
+ *
+ *   q, out   device [B, H_q, Q, d], Q <= 16
+ *   tables   device int [B, max_blocks];  lens  device int [B]
+ *   top_idx  device int [B, H_q, Q, k], k <= 64, or NULL with k = 0
+ *   ws       device workspace of saki_cache_attend_workspace_bytes(...) (k = 0),
+ *            16-byte aligned
+ * The time goes by the lengths on the device; max_blocks only bounds the workspace.
+ */
+int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q, int d,
+                      const void* k_cache, const void* v_cache, const float* scales,
+                      int n_blocks, const int* tables, int max_blocks, const int* lens,
+                      const int* top_idx, int k, void* out, void* ws, size_t ws_bytes,
+                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,3 +14,7 @@ therefore not reproduced here at all.
 """
 from .saki import *  # noqa: F401,F403
 from .saki import __all__  # noqa: F401
+from .serve import *  # noqa: F401,F403
+from .serve import __all__ as _serve_all
+
+__all__ = __all__ + _serve_all

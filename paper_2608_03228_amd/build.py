@@ -20,6 +20,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
+KERNELS = ("saki_kernels", "saki_serve")  # the index, and serving around it
 # Packed FP32 instructions are disabled for all device code.
 NO_PACKED_FP32 = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # MFMA results are written to the architectural VGPRs rather than the
@@ -38,15 +39,16 @@ def build(verbose: bool = True) -> str:
     """Compile every source and link libsaki.so; returns its path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     host_o = os.path.join(BUILD_DIR, "saki_host.o")
-    dev_o = os.path.join(BUILD_DIR, "saki_kernels.o")
+    dev_o = [os.path.join(BUILD_DIR, name + ".o") for name in KERNELS]
     _run(["g++", "-O3", "-std=c++17", "-fPIC", "-march=x86-64-v3", "-pthread",
           "-Wall", "-Wextra", "-I", INCLUDE, "-I", CSRC, "-c",
           os.path.join(CSRC, "saki_host.cpp"), "-o", host_o], verbose)
-    _run([HIPCC, "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", *NO_PACKED_FP32, *MFMA_VGPR,
-          "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, "saki_kernels.hip"),
-          "-o", dev_o], verbose)
+    for name, obj in zip(KERNELS, dev_o):
+        _run([HIPCC, "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", *NO_PACKED_FP32,
+              *MFMA_VGPR, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, name + ".hip"),
+              "-o", obj], verbose)
     tmp = LIB + ".tmp"
-    _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-pthread", host_o, dev_o,
+    _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-pthread", host_o, *dev_o,
           "-o", tmp], verbose)
     os.replace(tmp, LIB)
     return LIB

@@ -1,5 +1,5 @@
-// Wave-level running top-64 selection for gfx950 (wave64).  Device code,
-// included by saki_kernels.hip only.
+// Wave-level running top-64 selection for gfx950 (wave64), and the lane
+// shuffles it is made of.  Device code.
 //
 // Ranking: score descending, then key index ascending (ties go to the lower
 // index).  Both orders are folded into one integer key so that every

@@ -64,6 +64,13 @@ def lib():
                              sz, vp]),
         "saki_attend": (ip, [vp, ip, vp, vp, ip, ip, ip, ip, ip, ip, ip, ip, ip, ip, vp, vp, ip,
                              vp, vp, vp, ip, C.c_float, vp, vp]),
+        "saki_rope": (ip, [vp, vp, ip, ip, ip, ip, ip, sz, sz, vp, ip, vp, C.c_float, ip, vp, vp,
+                           sz, sz, vp]),
+        "saki_block_tables": (ip, [vp, vp, ip, vp, ip, vp, ip, vp, vp, ip, vp, vp, vp, vp]),
+        "saki_cache_write": (ip, [vp, vp, ip, ip, ip, ip, sz, sz, vp, vp, vp, vp, ip, vp]),
+        "saki_cache_attend_workspace_bytes": (sz, [ip, ip, ip, ip, ip, ip]),
+        "saki_cache_attend": (ip, [vp, ip, ip, ip, ip, ip, ip, vp, vp, vp, ip, vp, ip, vp, vp, ip,
+                                   vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -401,4 +408,201 @@ def saki_attend(values, q, top_idx, N_valid: int, keys=None, index=None, sketch:
         _dev(top_idx, (torch.int32,), "top_idx"), int(k), float(rope_theta),
         _dev(out, (torch.float32,), "out"), _stream(stream))
     _check("saki_attend", st)
+    return out
+
+
+# ------------------------------------------------------- serving around the index
+
+CACHE_BLOCK = 64    # tokens per cache block
+CACHE_MAX_Q = 16    # queries per request and head in saki_cache_attend
+
+
+def _float_type(t, name):
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise ValueError(f"{name} has dtype {t.dtype}, expected float32 or bfloat16")
+
+
+def _here(*tensors):
+    """The tensors (None is skipped) are on the current device, whose stream
+    the kernels run on."""
+    dev = _get_device() if _get_device is not None else _torch().cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"every tensor must be on the current device (cuda:{dev}), "
+                             f"one is on {t.device}")
+
+
+def _rows(t, name, like=None):
+    """Token rows [T, H, d] whose heads are dense -> (pointer, elements between
+    tokens).  `like`: (shape, dtype) to agree with."""
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [T, H, d]")
+    T, H, d = t.shape
+    if like is not None and ((T, H, d) != tuple(like[0]) or t.dtype != like[1]):
+        raise ValueError(f"{name} must be {tuple(like[0])} {like[1]}, got {(T, H, d)} {t.dtype}")
+    sT, sH, sd = t.stride()
+    if t.numel() == 0:
+        return t.data_ptr(), H * d
+    if (sd != 1 and d > 1) or (sH != d and H > 1) or (T > 1 and sT < H * d):
+        raise ValueError(f"{name} must have dense heads in rows that do not overlap, "
+                         f"got strides {(sT, sH, sd)}")
+    return t.data_ptr(), sT if T > 1 else H * d
+
+
+def _int_array(t, shape, name):
+    p = _dev(t, (_torch().int32,), name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return p
+
+
+def _cache_arrays(k_cache, v_cache, scales):
+    """-> pointers, n_blocks, H_kv, d"""
+    torch = _torch()
+    kp = _dev(k_cache, (torch.float8_e4m3fn,), "k_cache")
+    vp_ = _dev(v_cache, (torch.float8_e4m3fn,), "v_cache")
+    sp = _dev(scales, (torch.float32,), "scales")
+    if k_cache.dim() != 4 or k_cache.shape[2] != CACHE_BLOCK or v_cache.shape != k_cache.shape:
+        raise ValueError(f"k_cache and v_cache must be [n_blocks, H_kv, {CACHE_BLOCK}, d]")
+    n_blocks, H_kv, _, d = k_cache.shape
+    if tuple(scales.shape) != (n_blocks, H_kv, 2):
+        raise ValueError(f"scales must be [{n_blocks}, {H_kv}, 2]")
+    return kp, vp_, sp, n_blocks, H_kv, d
+
+
+def _used_on(stream, *tensors):
+    """Tensors allocated here, on the current stream, and used on `stream`."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse: bool = False,
+              q_out=None, k_out=None, stream=None):
+    """q [T, H_q, d], k [T, H_kv, d] (or None), float32 or bfloat16; pos [T] or
+    [axes, T] int32; sections: pairs of each axis (sum d/2; one axis needs
+    none).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    torch = _torch()
+    dt = _float_type(q, "q")
+    qp, ldq = _rows(q, "q")
+    T, H_q, d = q.shape
+    H_kv = k.shape[1] if k is not None else 0
+    kp, ldk = _rows(k, "k", ((T, H_kv, d), q.dtype)) if k is not None else (None, 0)
+    if pos.dim() == 1:
+        pos = pos[None]
+    axes = pos.shape[0]
+    pp = _int_array(pos, (axes, T), "pos")
+    if sections is None and axes == 1:
+        sections = (d // 2,)
+    if sections is None or len(sections) != axes:
+        raise ValueError("sections must give the pairs of each axis of pos")
+    if q_out is None:
+        q_out = torch.empty((T, H_q, d), dtype=q.dtype, device=q.device)
+        _used_on(stream, q_out)
+    if k is not None and k_out is None:
+        k_out = torch.empty((T, H_kv, d), dtype=q.dtype, device=q.device)
+        _used_on(stream, k_out)
+    qo, ldqo = _rows(q_out, "q_out", (q.shape, q.dtype))
+    ko, ldko = _rows(k_out, "k_out", (k.shape, q.dtype)) if k is not None else (None, 0)
+    _here(q, k, pos, q_out, k_out if k is not None else None)
+    st = lib().saki_rope(qp, kp, dt, T, H_q, H_kv, d, ldq, ldk, pp, axes,
+                         (C.c_int * axes)(*sections), float(rope_theta), int(bool(inverse)), qo, ko,
+                         ldqo, ldko, _stream(stream))
+    _check("saki_rope", st)
+    return q_out, k_out if k is not None else None
+
+
+def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=None, lens=None,
+                      counts=None, stream=None):
+    """ctx_lens, new_lens [B], free_blocks [n_free], tables [B, max_blocks] (in
+    place), slots and pos [T] (outputs), all int32 CUDA.  Returns (tables,
+    slots, pos, cu [B + 1], lens [B], counts [2])."""
+    torch = _torch()
+    if tables.dim() != 2 or slots.dim() != 1 or free_blocks.dim() != 1:
+        raise ValueError("tables must be [B, max_blocks], slots [T] and free_blocks [n_free]")
+    B, max_blocks = tables.shape
+    T, n_free = slots.shape[0], free_blocks.shape[0]
+    new = {"dtype": torch.int32, "device": tables.device}
+    if cu is None:
+        cu = torch.empty(B + 1, **new)
+        _used_on(stream, cu)
+    if lens is None:
+        lens = torch.empty(B, **new)
+        _used_on(stream, lens)
+    if counts is None:
+        counts = torch.empty(2, **new)
+        _used_on(stream, counts)
+    args = (_int_array(ctx_lens, (B,), "ctx_lens"), _int_array(new_lens, (B,), "new_lens"), B,
+            _int_array(free_blocks, (n_free,), "free_blocks"), n_free,
+            _int_array(tables, (B, max_blocks), "tables"), max_blocks,
+            _int_array(slots, (T,), "slots"), _int_array(pos, (T,), "pos"), T,
+            _int_array(cu, (B + 1,), "cu"), _int_array(lens, (B,), "lens"),
+            _int_array(counts, (2,), "counts"))
+    _here(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu, lens, counts)
+    _check("saki_block_tables", lib().saki_block_tables(*args, _stream(stream)))
+    return tables, slots, pos, cu, lens, counts
+
+
+def saki_cache_write(k, v, slots, k_cache, v_cache, scales, stream=None):
+    """k, v [T, H_kv, d] (float32 or bfloat16), slots [T] int32, to k_cache and
+    v_cache [n_blocks, H_kv, 64, d] (float8_e4m3fn) and scales [n_blocks, H_kv,
+    2] float32, in place.  Returns (k_cache, v_cache, scales)."""
+    dt = _float_type(k, "k")
+    kc, vc, sc, n_blocks, H_kv, d = _cache_arrays(k_cache, v_cache, scales)
+    T = k.shape[0]
+    kp, ldk = _rows(k, "k", ((T, H_kv, d), k.dtype))
+    vp_, ldv = _rows(v, "v", ((T, H_kv, d), k.dtype))
+    sp = _int_array(slots, (T,), "slots")
+    _here(k, v, slots, k_cache, v_cache, scales)
+    st = lib().saki_cache_write(kp, vp_, dt, T, H_kv, d, ldk, ldv, sp, kc, vc, sc, n_blocks,
+                                _stream(stream))
+    _check("saki_cache_write", st)
+    return k_cache, v_cache, scales
+
+
+def saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, k=0) -> int:
+    return int(lib().saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, k))
+
+
+def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, out=None, ws=None,
+                      stream=None):
+    """q [B, H_q, Q, d] (float32 or bfloat16), the cache of saki_cache_write,
+    tables [B, max_blocks] and lens [B] int32, top_idx [B, H_q, Q, k] int32 (the
+    listed keys only) or None (every key).  Returns out, as q."""
+    torch = _torch()
+    dt = _float_type(q, "q")
+    qp = _dev(q, (q.dtype,), "q")
+    if q.dim() != 4 or tables.dim() != 2:
+        raise ValueError("q must be [B, H_q, Q, d] and tables [B, max_blocks]")
+    B, H_q, Q, d = q.shape
+    kc, vc, sc, n_blocks, H_kv, dc = _cache_arrays(k_cache, v_cache, scales)
+    if dc != d:
+        raise ValueError(f"q has d = {d}, the cache {dc}")
+    max_blocks = tables.shape[1]
+    tp, lp = _int_array(tables, (B, max_blocks), "tables"), _int_array(lens, (B,), "lens")
+    k, ip = 0, None
+    if top_idx is not None:
+        k = top_idx.shape[-1]
+        ip = _int_array(top_idx, (B, H_q, Q, k), "top_idx")
+    if out is None:
+        out = torch.empty_like(q)
+        _used_on(stream, out)
+    op = _dev(out, (q.dtype,), "out")
+    if out.shape != q.shape:
+        raise ValueError(f"out must have q's shape {tuple(q.shape)}")
+    if ws is None and top_idx is None:
+        ws = torch.empty(max(saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks), 1),
+                         dtype=torch.uint8, device=q.device)
+        _used_on(stream, ws)
+    wp, wn = (_dev(ws, (torch.uint8,), "ws"), ws.numel()) if ws is not None else (None, 0)
+    _here(q, k_cache, v_cache, scales, tables, lens, top_idx, out, ws)
+    st = lib().saki_cache_attend(qp, dt, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
+                                 lp, ip, k, op, wp, wn, _stream(stream))
+    _check("saki_cache_attend", st)
     return out
