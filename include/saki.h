@@ -453,6 +453,21 @@ int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q,
                       const int* top_idx, int k, void* out, void* ws, size_t ws_bytes,
                       void* stream);
 
+/*
+ * saki_attend_prompt (GPU) -- causal attention of B packed prompts: token t of
+ * a prompt attends over the prompt's tokens up to itself,
+ *   out_t = sum_{u <= t} p_u value_u,  p = softmax(q_t . key_u / sqrt(d)),
+ * every query head over the keys of its group.  bf16 takes its products and
+ * weights in bf16 with float32 sums; float32 keeps float32 throughout.
+ *
+ *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v apart
+ *   cu      device int [B + 1], ascending: prompt b is tokens [cu[b], cu[b+1])
+ *   out     device [T, H_q, d], dense; tokens of no prompt are left as they were
+ */
+int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, int T, int B,
+                       int H_q, int H_kv, int d, size_t ld_q, size_t ld_k, size_t ld_v,
+                       const int* cu, void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

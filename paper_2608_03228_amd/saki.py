@@ -71,6 +71,7 @@ def lib():
         "saki_cache_attend_workspace_bytes": (sz, [ip, ip, ip, ip, ip, ip]),
         "saki_cache_attend": (ip, [vp, ip, ip, ip, ip, ip, ip, vp, vp, vp, ip, vp, ip, vp, vp, ip,
                                    vp, vp, sz, vp]),
+        "saki_attend_prompt": (ip, [vp, vp, vp, ip, ip, ip, ip, ip, ip, sz, sz, sz, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -605,4 +606,30 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
     st = lib().saki_cache_attend(qp, dt, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
                                  lp, ip, k, op, wp, wn, _stream(stream))
     _check("saki_cache_attend", st)
+    return out
+
+
+def saki_attend_prompt(q, k, v, cu, out=None, stream=None):
+    """q [T, H_q, d], k, v [T, H_kv, d] (float32 or bfloat16), cu [B + 1] int32:
+    causal attention within each of the packed prompts.  Returns out [T, H_q, d]."""
+    torch = _torch()
+    dt = _float_type(q, "q")
+    qp, ldq = _rows(q, "q")
+    T, H_q, d = q.shape
+    H_kv = k.shape[1]
+    kp, ldk = _rows(k, "k", ((T, H_kv, d), q.dtype))
+    vp_, ldv = _rows(v, "v", ((T, H_kv, d), q.dtype))
+    if cu.dim() != 1 or cu.shape[0] < 1:
+        raise ValueError("cu must be [B + 1]")
+    cp = _int_array(cu, tuple(cu.shape), "cu")
+    if out is None:
+        out = torch.empty((T, H_q, d), dtype=q.dtype, device=q.device)
+        _used_on(stream, out)
+    op = _dev(out, (q.dtype,), "out")
+    if tuple(out.shape) != (T, H_q, d):
+        raise ValueError(f"out must be {(T, H_q, d)}")
+    _here(q, k, v, cu, out)
+    st = lib().saki_attend_prompt(qp, kp, vp_, dt, T, cu.shape[0] - 1, H_q, H_kv, d, ldq, ldk, ldv,
+                                  cp, op, _stream(stream))
+    _check("saki_attend_prompt", st)
     return out

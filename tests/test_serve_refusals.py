@@ -96,6 +96,20 @@ def test_cache_attend_workspace():
     assert f(1, 4, 1, 1, 1, 65) == 0
 
 
+PROMPT = "q k v dtype T B H_q H_kv d ld_q ld_k ld_v cu out stream".split()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=0), 0), (dict(B=0), 0), (dict(T=-1), ARG), (dict(B=-1), ARG), (dict(H_q=3), ARG), (dict(H_kv=0), ARG),
+    (dict(d=0), ARG), (dict(d=64), UNSUP), (dict(dtype=2), UNSUP), (dict(T=1 << 30), UNSUP),
+    (dict(B=1 << 30), UNSUP), (dict(q=None), ARG), (dict(k=ODD), ARG), (dict(v=None), ARG), (dict(out=None), ARG),
+    (dict(out=ODD), ARG), (dict(cu=None), ARG), (dict(ld_q=511), ARG), (dict(ld_k=128), ARG), (dict(ld_v=260), ARG),
+])
+def test_attend_prompt(lib, kw, status):
+    good = [P, P, P, 1, 5, 2, 4, 2, 128, 512, 256, 256, P, P, None]
+    assert change(lib.saki_attend_prompt, good, PROMPT, **kw) == status
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros(2, 4, 128)
     i = torch.zeros(2, dtype=torch.int32)
@@ -109,3 +123,5 @@ def test_binding_refuses_host_tensors():
         S.saki_cache_write(x, x, i, c, c, s)
     with pytest.raises(ValueError):
         S.saki_cache_attend(torch.zeros(1, 4, 1, 128), c, c, s, i[None], i[:1])
+    with pytest.raises(ValueError):
+        S.saki_attend_prompt(x, x, x, i)
