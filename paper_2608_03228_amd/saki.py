@@ -417,71 +417,107 @@ def saki_attend(values, q, top_idx, N_valid: int, keys=None, index=None, sketch:
 CACHE_BLOCK = 64    # tokens per cache block
 CACHE_MAX_Q = 16    # queries per request and head in saki_cache_attend
 
+# These calls run 4 to 10 us on the GPU for a decode step, as long as a dozen
+# checked arguments take in Python; so each argument is checked once, by as few
+# attribute reads as tell that it is right, and looked at again only to say
+# what is wrong with it (10.4 us a call before, see the checks below).
 
-def _float_type(t, name):
+
+def _current():
+    """The current device's index and its current stream."""
     torch = _torch()
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise ValueError(f"{name} has dtype {t.dtype}, expected float32 or bfloat16")
+    if _raw_stream is not None and _get_device is not None:
+        dev = _get_device()
+        return torch, dev, _raw_stream(dev)
+    return torch, torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream
 
 
-def _here(*tensors):
-    """The tensors (None is skipped) are on the current device, whose stream
-    the kernels run on."""
-    dev = _get_device() if _get_device is not None else _torch().cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"every tensor must be on the current device (cuda:{dev}), "
-                             f"one is on {t.device}")
-
-
-def _rows(t, name, like=None):
-    """Token rows [T, H, d] whose heads are dense -> (pointer, elements between
-    tokens).  `like`: (shape, dtype) to agree with."""
+def _array(t, dtype, shape, dev, name):
+    """A dense tensor of this type and shape on the current device -> pointer."""
+    try:
+        if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [T, H, d]")
-    T, H, d = t.shape
-    if like is not None and ((T, H, d) != tuple(like[0]) or t.dtype != like[1]):
-        raise ValueError(f"{name} must be {tuple(like[0])} {like[1]}, got {(T, H, d)} {t.dtype}")
-    sT, sH, sd = t.stride()
-    if t.numel() == 0:
-        return t.data_ptr(), H * d
-    if (sd != 1 and d > 1) or (sH != d and H > 1) or (T > 1 and sT < H * d):
-        raise ValueError(f"{name} must have dense heads in rows that do not overlap, "
-                         f"got strides {(sT, sH, sd)}")
-    return t.data_ptr(), sT if T > 1 else H * d
-
-
-def _int_array(t, shape, name):
-    p = _dev(t, (_torch().int32,), name)
-    if tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current device (cuda:{dev})")
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return p
+    raise ValueError(f"{name} must be contiguous")
 
 
-def _cache_arrays(k_cache, v_cache, scales):
+def _rows(t, dtype, shape, dev, name):
+    """Token rows [T, H, d] whose heads are dense -> pointer, elements between tokens."""
+    T, H, d = shape
+    try:
+        if t.dtype is dtype and t.get_device() == dev and t.shape == shape:
+            if t.is_contiguous():
+                return t.data_ptr(), H * d
+            sT, sH, sd = t.stride()
+            if (sd == 1 or d == 1) and (sH == d or H == 1) and (sT >= H * d or T == 1):
+                return t.data_ptr(), sT if T > 1 else H * d
+            raise ValueError(f"{name} must have dense heads in rows that do not overlap, got "
+                             f"strides {(sT, sH, sd)}")
+    except AttributeError:
+        pass
+    return _array(t, dtype, shape, dev, name), H * d
+
+
+def _of_floats(t, dims, name):
+    """-> shape, torch dtype and library dtype of a float32 or bf16 tensor."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    dt = t.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise ValueError(f"{name} has dtype {dt}, expected float32 or bfloat16")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+    return t.shape, dt, BF16 if dt is torch.bfloat16 else F32
+
+
+def _cache_arrays(k_cache, v_cache, scales, dev):
     """-> pointers, n_blocks, H_kv, d"""
     torch = _torch()
-    kp = _dev(k_cache, (torch.float8_e4m3fn,), "k_cache")
-    vp_ = _dev(v_cache, (torch.float8_e4m3fn,), "v_cache")
-    sp = _dev(scales, (torch.float32,), "scales")
-    if k_cache.dim() != 4 or k_cache.shape[2] != CACHE_BLOCK or v_cache.shape != k_cache.shape:
-        raise ValueError(f"k_cache and v_cache must be [n_blocks, H_kv, {CACHE_BLOCK}, d]")
-    n_blocks, H_kv, _, d = k_cache.shape
-    if tuple(scales.shape) != (n_blocks, H_kv, 2):
-        raise ValueError(f"scales must be [{n_blocks}, {H_kv}, 2]")
-    return kp, vp_, sp, n_blocks, H_kv, d
+    shape = k_cache.shape
+    if len(shape) != 4 or shape[2] != CACHE_BLOCK:
+        raise ValueError(f"k_cache must be [n_blocks, H_kv, {CACHE_BLOCK}, d]")
+    n_blocks, H_kv, _, d = shape
+    f8 = torch.float8_e4m3fn
+    return (_array(k_cache, f8, shape, dev, "k_cache"), _array(v_cache, f8, shape, dev, "v_cache"),
+            _array(scales, torch.float32, (n_blocks, H_kv, 2), dev, "scales"), n_blocks, H_kv, d)
 
 
-def _used_on(stream, *tensors):
-    """Tensors allocated here, on the current stream, and used on `stream`."""
+def _new(stream, shape, dtype, dev):
+    """A tensor that the call writes or works in: allocated on the current
+    stream, marked as used on `stream`."""
+    torch = _torch()
+    t = torch.empty(shape, dtype=dtype, device=dev)
     if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+        t.record_stream(stream)
+    return t
+
+
+_section_arrays = {}
+
+
+def _sections(sections, axes, d):
+    """The host array of the sections (one per distinct tuple, at most 256)."""
+    if sections is None and axes == 1:
+        sections = (d // 2,)
+    if sections is None or len(sections) != axes:
+        raise ValueError("sections must give the pairs of each axis of pos")
+    key = tuple(sections)
+    a = _section_arrays.get(key)
+    if a is None:
+        a = (C.c_int * axes)(*key)
+        if len(_section_arrays) < 256:
+            _section_arrays[key] = a
+    return a
 
 
 def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse: bool = False,
@@ -489,34 +525,36 @@ def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse:
     """q [T, H_q, d], k [T, H_kv, d] (or None), float32 or bfloat16; pos [T] or
     [axes, T] int32; sections: pairs of each axis (sum d/2; one axis needs
     none).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
-    torch = _torch()
-    dt = _float_type(q, "q")
-    qp, ldq = _rows(q, "q")
-    T, H_q, d = q.shape
-    H_kv = k.shape[1] if k is not None else 0
-    kp, ldk = _rows(k, "k", ((T, H_kv, d), q.dtype)) if k is not None else (None, 0)
+    shape, dt, code = _of_floats(q, 3, "q")
+    torch, dev, cur = _current()
+    T, H_q, d = shape
+    qp, ldq = _rows(q, dt, shape, dev, "q")
     if pos.dim() == 1:
-        pos = pos[None]
-    axes = pos.shape[0]
-    pp = _int_array(pos, (axes, T), "pos")
-    if sections is None and axes == 1:
-        sections = (d // 2,)
-    if sections is None or len(sections) != axes:
-        raise ValueError("sections must give the pairs of each axis of pos")
+        axes, pp = 1, _array(pos, torch.int32, (T,), dev, "pos")
+    else:
+        axes = pos.shape[0]
+        pp = _array(pos, torch.int32, (axes, T), dev, "pos")
+    sec = _sections(sections, axes, d)
     if q_out is None:
-        q_out = torch.empty((T, H_q, d), dtype=q.dtype, device=q.device)
-        _used_on(stream, q_out)
-    if k is not None and k_out is None:
-        k_out = torch.empty((T, H_kv, d), dtype=q.dtype, device=q.device)
-        _used_on(stream, k_out)
-    qo, ldqo = _rows(q_out, "q_out", (q.shape, q.dtype))
-    ko, ldko = _rows(k_out, "k_out", (k.shape, q.dtype)) if k is not None else (None, 0)
-    _here(q, k, pos, q_out, k_out if k is not None else None)
-    st = lib().saki_rope(qp, kp, dt, T, H_q, H_kv, d, ldq, ldk, pp, axes,
-                         (C.c_int * axes)(*sections), float(rope_theta), int(bool(inverse)), qo, ko,
-                         ldqo, ldko, _stream(stream))
-    _check("saki_rope", st)
-    return q_out, k_out if k is not None else None
+        q_out = _new(stream, shape, dt, q.device)
+    qo, ldqo = (qp, ldq) if q_out is q else _rows(q_out, dt, shape, dev, "q_out")
+    H_kv = ldk = ldko = 0
+    kp = ko = None
+    if k is not None:
+        H_kv = k.shape[1]
+        kshape = (T, H_kv, d)
+        kp, ldk = _rows(k, dt, kshape, dev, "k")
+        if k_out is None:
+            k_out = _new(stream, kshape, dt, q.device)
+        ko, ldko = (kp, ldk) if k_out is k else _rows(k_out, dt, kshape, dev, "k_out")
+    else:
+        k_out = None
+    st = lib().saki_rope(qp, kp, code, T, H_q, H_kv, d, ldq, ldk, pp, axes, sec, rope_theta,
+                         1 if inverse else 0, qo, ko, ldqo, ldko,
+                         cur if stream is None else stream.cuda_stream)
+    if st:
+        _check("saki_rope", st)
+    return q_out, k_out
 
 
 def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=None, lens=None,
@@ -524,29 +562,29 @@ def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=No
     """ctx_lens, new_lens [B], free_blocks [n_free], tables [B, max_blocks] (in
     place), slots and pos [T] (outputs), all int32 CUDA.  Returns (tables,
     slots, pos, cu [B + 1], lens [B], counts [2])."""
-    torch = _torch()
+    if not tables.is_cuda:
+        raise ValueError("tables must be a CUDA (HIP) tensor")
+    torch, dev, cur = _current()
+    i32 = torch.int32
     if tables.dim() != 2 or slots.dim() != 1 or free_blocks.dim() != 1:
         raise ValueError("tables must be [B, max_blocks], slots [T] and free_blocks [n_free]")
     B, max_blocks = tables.shape
     T, n_free = slots.shape[0], free_blocks.shape[0]
-    new = {"dtype": torch.int32, "device": tables.device}
     if cu is None:
-        cu = torch.empty(B + 1, **new)
-        _used_on(stream, cu)
+        cu = _new(stream, (B + 1,), i32, tables.device)
     if lens is None:
-        lens = torch.empty(B, **new)
-        _used_on(stream, lens)
+        lens = _new(stream, (B,), i32, tables.device)
     if counts is None:
-        counts = torch.empty(2, **new)
-        _used_on(stream, counts)
-    args = (_int_array(ctx_lens, (B,), "ctx_lens"), _int_array(new_lens, (B,), "new_lens"), B,
-            _int_array(free_blocks, (n_free,), "free_blocks"), n_free,
-            _int_array(tables, (B, max_blocks), "tables"), max_blocks,
-            _int_array(slots, (T,), "slots"), _int_array(pos, (T,), "pos"), T,
-            _int_array(cu, (B + 1,), "cu"), _int_array(lens, (B,), "lens"),
-            _int_array(counts, (2,), "counts"))
-    _here(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu, lens, counts)
-    _check("saki_block_tables", lib().saki_block_tables(*args, _stream(stream)))
+        counts = _new(stream, (2,), i32, tables.device)
+    st = lib().saki_block_tables(
+        _array(ctx_lens, i32, (B,), dev, "ctx_lens"), _array(new_lens, i32, (B,), dev, "new_lens"),
+        B, _array(free_blocks, i32, (n_free,), dev, "free_blocks"), n_free,
+        _array(tables, i32, (B, max_blocks), dev, "tables"), max_blocks,
+        _array(slots, i32, (T,), dev, "slots"), _array(pos, i32, (T,), dev, "pos"), T,
+        _array(cu, i32, (B + 1,), dev, "cu"), _array(lens, i32, (B,), dev, "lens"),
+        _array(counts, i32, (2,), dev, "counts"), cur if stream is None else stream.cuda_stream)
+    if st:
+        _check("saki_block_tables", st)
     return tables, slots, pos, cu, lens, counts
 
 
@@ -554,16 +592,18 @@ def saki_cache_write(k, v, slots, k_cache, v_cache, scales, stream=None):
     """k, v [T, H_kv, d] (float32 or bfloat16), slots [T] int32, to k_cache and
     v_cache [n_blocks, H_kv, 64, d] (float8_e4m3fn) and scales [n_blocks, H_kv,
     2] float32, in place.  Returns (k_cache, v_cache, scales)."""
-    dt = _float_type(k, "k")
-    kc, vc, sc, n_blocks, H_kv, d = _cache_arrays(k_cache, v_cache, scales)
+    _, dt, code = _of_floats(k, 3, "k")
+    torch, dev, cur = _current()
+    kc, vc, sc, n_blocks, H_kv, d = _cache_arrays(k_cache, v_cache, scales, dev)
     T = k.shape[0]
-    kp, ldk = _rows(k, "k", ((T, H_kv, d), k.dtype))
-    vp_, ldv = _rows(v, "v", ((T, H_kv, d), k.dtype))
-    sp = _int_array(slots, (T,), "slots")
-    _here(k, v, slots, k_cache, v_cache, scales)
-    st = lib().saki_cache_write(kp, vp_, dt, T, H_kv, d, ldk, ldv, sp, kc, vc, sc, n_blocks,
-                                _stream(stream))
-    _check("saki_cache_write", st)
+    shape = (T, H_kv, d)
+    kp, ldk = _rows(k, dt, shape, dev, "k")
+    vp_, ldv = _rows(v, dt, shape, dev, "v")
+    st = lib().saki_cache_write(kp, vp_, code, T, H_kv, d, ldk, ldv,
+                                _array(slots, torch.int32, (T,), dev, "slots"), kc, vc, sc, n_blocks,
+                                cur if stream is None else stream.cuda_stream)
+    if st:
+        _check("saki_cache_write", st)
     return k_cache, v_cache, scales
 
 
@@ -576,60 +616,59 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
     """q [B, H_q, Q, d] (float32 or bfloat16), the cache of saki_cache_write,
     tables [B, max_blocks] and lens [B] int32, top_idx [B, H_q, Q, k] int32 (the
     listed keys only) or None (every key).  Returns out, as q."""
-    torch = _torch()
-    dt = _float_type(q, "q")
-    qp = _dev(q, (q.dtype,), "q")
-    if q.dim() != 4 or tables.dim() != 2:
-        raise ValueError("q must be [B, H_q, Q, d] and tables [B, max_blocks]")
-    B, H_q, Q, d = q.shape
-    kc, vc, sc, n_blocks, H_kv, dc = _cache_arrays(k_cache, v_cache, scales)
+    shape, dt, code = _of_floats(q, 4, "q")
+    torch, dev, cur = _current()
+    B, H_q, Q, d = shape
+    qp = _array(q, dt, shape, dev, "q")
+    kc, vc, sc, n_blocks, H_kv, dc = _cache_arrays(k_cache, v_cache, scales, dev)
     if dc != d:
         raise ValueError(f"q has d = {d}, the cache {dc}")
+    if tables.dim() != 2:
+        raise ValueError("tables must be [B, max_blocks]")
     max_blocks = tables.shape[1]
-    tp, lp = _int_array(tables, (B, max_blocks), "tables"), _int_array(lens, (B,), "lens")
-    k, ip = 0, None
+    tp = _array(tables, torch.int32, (B, max_blocks), dev, "tables")
+    lp = _array(lens, torch.int32, (B,), dev, "lens")
+    if out is None:
+        out = _new(stream, shape, dt, q.device)
+    op = _array(out, dt, shape, dev, "out")
+    k = wn = 0
+    ip = wp = None
     if top_idx is not None:
         k = top_idx.shape[-1]
-        ip = _int_array(top_idx, (B, H_q, Q, k), "top_idx")
-    if out is None:
-        out = torch.empty_like(q)
-        _used_on(stream, out)
-    op = _dev(out, (q.dtype,), "out")
-    if out.shape != q.shape:
-        raise ValueError(f"out must have q's shape {tuple(q.shape)}")
-    if ws is None and top_idx is None:
-        ws = torch.empty(max(saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks), 1),
-                         dtype=torch.uint8, device=q.device)
-        _used_on(stream, ws)
-    wp, wn = (_dev(ws, (torch.uint8,), "ws"), ws.numel()) if ws is not None else (None, 0)
-    _here(q, k_cache, v_cache, scales, tables, lens, top_idx, out, ws)
-    st = lib().saki_cache_attend(qp, dt, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
-                                 lp, ip, k, op, wp, wn, _stream(stream))
-    _check("saki_cache_attend", st)
+        ip = _array(top_idx, torch.int32, (B, H_q, Q, k), dev, "top_idx")
+    else:
+        if ws is None:
+            need = saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks)
+            ws = _new(stream, max(need, 1), torch.uint8, q.device)
+        wn = ws.numel()
+        wp = _array(ws, torch.uint8, (wn,), dev, "ws")
+    st = lib().saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
+                                 lp, ip, k, op, wp, wn, cur if stream is None else stream.cuda_stream)
+    if st:
+        _check("saki_cache_attend", st)
     return out
 
 
 def saki_attend_prompt(q, k, v, cu, out=None, stream=None):
     """q [T, H_q, d], k, v [T, H_kv, d] (float32 or bfloat16), cu [B + 1] int32:
     causal attention within each of the packed prompts.  Returns out [T, H_q, d]."""
-    torch = _torch()
-    dt = _float_type(q, "q")
-    qp, ldq = _rows(q, "q")
-    T, H_q, d = q.shape
+    shape, dt, code = _of_floats(q, 3, "q")
+    torch, dev, cur = _current()
+    T, H_q, d = shape
     H_kv = k.shape[1]
-    kp, ldk = _rows(k, "k", ((T, H_kv, d), q.dtype))
-    vp_, ldv = _rows(v, "v", ((T, H_kv, d), q.dtype))
-    if cu.dim() != 1 or cu.shape[0] < 1:
+    kshape = (T, H_kv, d)
+    qp, ldq = _rows(q, dt, shape, dev, "q")
+    kp, ldk = _rows(k, dt, kshape, dev, "k")
+    vp_, ldv = _rows(v, dt, kshape, dev, "v")
+    n = cu.shape[0] if cu.dim() == 1 else 0
+    if n < 1:
         raise ValueError("cu must be [B + 1]")
-    cp = _int_array(cu, tuple(cu.shape), "cu")
+    cp = _array(cu, torch.int32, (n,), dev, "cu")
     if out is None:
-        out = torch.empty((T, H_q, d), dtype=q.dtype, device=q.device)
-        _used_on(stream, out)
-    op = _dev(out, (q.dtype,), "out")
-    if tuple(out.shape) != (T, H_q, d):
-        raise ValueError(f"out must be {(T, H_q, d)}")
-    _here(q, k, v, cu, out)
-    st = lib().saki_attend_prompt(qp, kp, vp_, dt, T, cu.shape[0] - 1, H_q, H_kv, d, ldq, ldk, ldv,
-                                  cp, op, _stream(stream))
-    _check("saki_attend_prompt", st)
+        out = _new(stream, shape, dt, q.device)
+    st = lib().saki_attend_prompt(qp, kp, vp_, code, T, n - 1, H_q, H_kv, d, ldq, ldk, ldv, cp,
+                                  _array(out, dt, shape, dev, "out"),
+                                  cur if stream is None else stream.cuda_stream)
+    if st:
+        _check("saki_attend_prompt", st)
     return out
