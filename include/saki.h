@@ -453,20 +453,29 @@ int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q,
                       const int* top_idx, int k, void* out, void* ws, size_t ws_bytes,
                       void* stream);
 
+/* Workspace for saki_attend_prompt (bytes; 0 on bad arguments): for float32 the
+ * parts of the keys and values, about as many bytes as those. */
+size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv);
+
 /*
  * saki_attend_prompt (GPU) -- causal attention of B packed prompts: token t of
  * a prompt attends over the prompt's tokens up to itself,
  *   out_t = sum_{u <= t} p_u value_u,  p = softmax(q_t . key_u / sqrt(d)),
- * every query head over the keys of its group.  bf16 takes its products and
- * weights in bf16 with float32 sums; float32 keeps float32 throughout.
+ * every query head over the keys of its group.  Sums and softmax are float32.
+ * bf16 inputs meet in exact products, and the weights are rounded to bf16 for
+ * theirs.  float32 elements and weights are taken as two fp16 parts with a
+ * common power of two for 32 tokens (or one query): 22 bits of each, products
+ * to 2^-21.
  *
  *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v apart
  *   cu      device int [B + 1], ascending: prompt b is tokens [cu[b], cu[b+1])
  *   out     device [T, H_q, d], dense; tokens of no prompt are left as they were
+ *   ws      device workspace of saki_attend_prompt_workspace_bytes(...), 16-byte
+ *           aligned (float32; bf16 needs none and ws may be NULL)
  */
 int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, int T, int B,
                        int H_q, int H_kv, int d, size_t ld_q, size_t ld_k, size_t ld_v,
-                       const int* cu, void* out, void* stream);
+                       const int* cu, void* out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

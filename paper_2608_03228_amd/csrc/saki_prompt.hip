@@ -1,7 +1,8 @@
 // Causal attention of whole prompts for gfx950 (CDNA4, wave64):
 //
-//   prompt_attend_kernel  bf16, on the 32x32x16 MFMA
-//   prompt_attend_f32_kernel  float32, on the 32x32x2 MFMA
+//   prompt_attend_kernel      bf16
+//   prompt_split_kernel       float32 keys and values as pairs of fp16 parts
+//   prompt_attend_f32_kernel  float32 on those parts
 
 #include <hip/hip_runtime.h>
 
@@ -19,7 +20,7 @@ using saki::kHeadDim;
 using saki_dev::kWave;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
@@ -211,12 +212,113 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
   }
 }
 
-// float32: the same with every product on the float32 MFMA.  A work-group's
-// waves hold their queries in LDS-free registers; keys and values are staged
-// as rows of 128 floats.
-constexpr int kKeysF32 = 32;
-__global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a) {
-  __shared__ alignas(16) float lds[2][2][kKeysF32][kHeadDim + 4];
+// float32 on the fp16 MFMA: x = (hi + lo) 2^-e with hi = fp16(x 2^e), lo = fp16(x
+// 2^e - hi), where 2^e brings the largest element of a tile (of a query's row)
+// to [2^14, 2^15).  What hi and lo leave is below 2^-22 |x|, or 2^-39 of that
+// largest element, and a product is hi hi + lo hi + hi lo, all sums in float32:
+// three fp16 products in place of one at an eighth of their rate.
+
+constexpr int kSplitKeys = 32;
+constexpr int kSplitTile = 4 * kSplitKeys * kHeadDim * 2;  // bytes: keys hi, lo, values hi, lo
+
+__device__ __forceinline__ float ldexp_f32(float x, int e) { return __builtin_amdgcn_ldexpf(x, e); }
+
+// e with top 2^e in [2^14, 2^15).
+__device__ __forceinline__ int unit_exponent(float top, int of_zero) {
+  return top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : of_zero;
+}
+
+// Eight floats times 2^e as hi and lo parts.
+__device__ __forceinline__ void split_f16(const float* x, int e, f16x8_t* hi, f16x8_t* lo) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float y = ldexp_f32(x[j], e);
+    (*hi)[j] = (_Float16)y;
+    (*lo)[j] = (_Float16)(y - (float)(*hi)[j]);
+  }
+}
+
+// Tile x of the packed prompts' keys (32 of one prompt; the tiles of prompt b
+// start at cu[b] / 32 + b): hi and lo parts of keys and values in the order in
+// which the lanes of prompt_attend_f32_kernel take them as operands, and the
+// exponents.  Reads each element once, writes as many bytes: HBM bound.
+__global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t* __restrict__ ws,
+                                                           int2* __restrict__ exps) {
+  __shared__ float part[2][4];
+  __shared__ float vals[kSplitKeys][kHeadDim + 4];
+  const int hk = blockIdx.x % a.H_kv, tile = blockIdx.x / a.H_kv;
+  int lo_b = 0, hi_b = a.B;
+  auto at = [&](int b) { return min(max(a.cu[b], 0), a.T); };
+  while (hi_b - lo_b > 1) {
+    const int mid = (lo_b + hi_b) >> 1;
+    if (at(mid) / kSplitKeys + mid <= tile)
+      lo_b = mid;
+    else
+      hi_b = mid;
+  }
+  const int start = at(lo_b), len = at(lo_b + 1) - start;
+  const int key0 = (tile - (start / kSplitKeys + lo_b)) * kSplitKeys;
+  if (key0 < 0 || key0 >= len) return;
+  const int tid = threadIdx.x, row = tid / 8, c = tid % 8 * 16;
+  float k[16], v[16];
+  const bool in = key0 + row < len;
+  const size_t tok = (size_t)(start + min(key0 + row, len - 1));
+  const float* kp = (const float*)a.k + tok * a.ld_k + (size_t)hk * kHeadDim + c;
+  const float* vp = (const float*)a.v + tok * a.ld_v + (size_t)hk * kHeadDim + c;
+  float kt = 0.f, vt = 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(kp + j), y = *reinterpret_cast<const float4*>(vp + j);
+    k[j] = x.x, k[j + 1] = x.y, k[j + 2] = x.z, k[j + 3] = x.w;
+    v[j] = y.x, v[j + 1] = y.y, v[j + 2] = y.z, v[j + 3] = y.w;
+  }
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    if (!in) k[j] = v[j] = 0.f;
+    kt = fmaxf(kt, fabsf(k[j]));
+    vt = fmaxf(vt, fabsf(v[j]));
+  }
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(&vals[row][c + j]) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    kt = fmaxf(kt, __shfl_xor(kt, m));
+    vt = fmaxf(vt, __shfl_xor(vt, m));
+  }
+  if (tid % kWave == 0) part[0][tid / kWave] = kt, part[1][tid / kWave] = vt;
+  __syncthreads();
+  const int ek = unit_exponent(fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3])), 0);
+  const int ev = unit_exponent(fmaxf(fmaxf(part[1][0], part[1][1]), fmaxf(part[1][2], part[1][3])), 200);  // zeros scale nothing down
+  const size_t id = (size_t)tile * a.H_kv + hk;
+  if (tid == 0) exps[id] = make_int2(ek, ev);
+  uint8_t* out = ws + id * kSplitTile;
+  constexpr int kPart = kSplitTile / 4;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {  // dims 16 x + 8 h of key `row`: step x = c / 16, lane 32 h + row
+    f16x8_t hi, lo;
+    split_f16(k + 8 * u, ek, &hi, &lo);
+    const int to = (c / 16) * 1024 + (32 * u + row) * 16;
+    __builtin_memcpy(out + to, &hi, 16);
+    __builtin_memcpy(out + kPart + to, &lo, 16);
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {  // step x = u, dim block d: lane 32 h + (dim % 32) holds keys 16 x + 4 h + {0..3, 8..11}
+    const int d = tid / 64, lane = tid % 64, h = lane / 32;
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = vals[16 * u + 4 * h + j % 4 + 8 * (j / 4)][32 * d + lane % 32];
+    f16x8_t hi, lo;
+    split_f16(y, ev, &hi, &lo);
+    const int to = (4 * u + d) * 1024 + lane * 16;
+    __builtin_memcpy(out + 2 * kPart + to, &hi, 16);
+    __builtin_memcpy(out + 3 * kPart + to, &lo, 16);
+  }
+}
+
+__global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
+                                                                   const int2* __restrict__ exps) {
+  __shared__ alignas(1024) uint8_t lds[2][kSplitTile];
+  constexpr int kPart = kSplitTile / 4;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
   const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv));
@@ -225,87 +327,105 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a)
   const int n = lane % 32, h = lane / 32;
   const int row = min(wave * 32 + n, n_rows - 1) + blk.row0;
   const int pos = row / G;
-  const size_t q_at = (size_t)(blk.start + pos) * a.ld_q + (size_t)(hk * G + row % G) * kHeadDim;
-  // dims 8 x + 4 h .. + 3 for x = 0 .. 15
-  float4 q[16];
+  const float* qp = (const float*)a.q + (size_t)(blk.start + pos) * a.ld_q + (size_t)(hk * G + row % G) * kHeadDim;
+  f16x8_t qh[8], ql[8];
+  int eq;
+  {
+    float x[64], top = 0.f;  // dims 16 s + 8 h .. + 7
 #pragma unroll
-  for (int x = 0; x < 16; ++x) q[x] = *reinterpret_cast<const float4*>((const float*)a.q + q_at + 8 * x + 4 * h);
+    for (int s = 0; s < 16; ++s) {
+      const float4 v = *reinterpret_cast<const float4*>(qp + 16 * (s / 2) + 8 * h + 4 * (s % 2));
+      x[4 * s] = v.x, x[4 * s + 1] = v.y, x[4 * s + 2] = v.z, x[4 * s + 3] = v.w;
+    }
+#pragma unroll
+    for (int j = 0; j < 64; ++j) top = fmaxf(top, fabsf(x[j]));
+    eq = unit_exponent(fmaxf(top, swap32(top)), 0);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) split_f16(x + 8 * s, eq, &qh[s], &ql[s]);
+  }
   const int pos_lo = (blk.row0 + min(wave * 32, n_rows - 1)) / G;
   const int pos_hi = (blk.row0 + min(wave * 32 + 31, n_rows - 1)) / G;
-  const int n_tiles = (blk.row0 + n_rows - 1) / G / kKeysF32 + 1;
-  const float* kp = (const float*)a.k + (size_t)blk.start * a.ld_k + (size_t)hk * kHeadDim;
-  const float* vp = (const float*)a.v + (size_t)blk.start * a.ld_v + (size_t)hk * kHeadDim;
-  float4 kx[4], vx[4];
-  const int sr = threadIdx.x / 32, sc = threadIdx.x % 32 * 4;
-  auto load = [&](int t) {
+  const int n_tiles = (blk.row0 + n_rows - 1) / G / kSplitKeys + 1;
+  const size_t tile0 = ((size_t)(blk.start / kSplitKeys + blk.b)) * a.H_kv + hk;
+  auto stage = [&](int t, int buf) {
+    const uint8_t* p = ws + (tile0 + (size_t)t * a.H_kv) * kSplitTile + wave * 8192 + lane * 16;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int tok = min(t * kKeysF32 + sr + 8 * u, blk.len - 1);
-      kx[u] = *reinterpret_cast<const float4*>(kp + (size_t)tok * a.ld_k + sc);
-      vx[u] = *reinterpret_cast<const float4*>(vp + (size_t)tok * a.ld_v + sc);
-    }
+    for (int u = 0; u < 8; ++u)
+      __builtin_amdgcn_global_load_lds((global_void*)(p + u * 1024), (lds_void*)(lds[buf] + wave * 8192 + u * 1024), 16,
+                                       0, 0);
   };
-  auto put = [&](int buf) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      *reinterpret_cast<float4*>(&lds[buf][0][sr + 8 * u][sc]) = kx[u];
-      *reinterpret_cast<float4*>(&lds[buf][1][sr + 8 * u][sc]) = vx[u];
-    }
-  };
+
   f32x16_t o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  // m: the running maximum in powers of two; o and l hold sums of 2^14 p (and o
+  // of values times 2^E, E the least exponent of the tiles so far)
   float m = -INFINITY, l = 0.f;
-  load(0);
-  put(0);
+  int E = INT_MAX;
+  stage(0, 0);
   for (int t = 0; t < n_tiles; ++t) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile t
     __syncthreads();
-    if (t + 1 < n_tiles) load(t + 1);
-    if (t * kKeysF32 <= pos_hi) {
-      const auto& kt = lds[t & 1][0];
-      const auto& vt = lds[t & 1][1];
-      f32x16_t s;
+    if (t + 1 < n_tiles) stage(t + 1, (t + 1) & 1);
+    if (t * kSplitKeys > pos_hi) continue;
+    const int2 ex = exps[tile0 + (size_t)t * a.H_kv];
+    const uint8_t* kt = lds[t & 1] + lane * 16;
+    f32x16_t s;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const float4 kf = *reinterpret_cast<const float4*>(&kt[n][8 * x + 4 * h]);
-        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.x, q[x].x, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.y, q[x].y, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.z, q[x].z, s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf.w, q[x].w, s, 0, 0, 0);
-      }
-      if (t * kKeysF32 + kKeysF32 - 1 > pos_lo) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t * kKeysF32 + 8 * (i / 4) + 4 * h + i % 4 > pos) s[i] = -INFINITY;
-      }
-      float top = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      top = fmaxf(top, swap32(top));
-      if (__any(top > m)) {
-        const float m1 = fmaxf(m, top);
-        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m1) * (kScale * kLog2e));
-        m = m1;
-        l *= keep;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[d] *= keep;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f((s[i] - m) * (kScale * kLog2e));
-        l += s[i];
-      }
+    for (int x = 0; x < 8; ++x) {
+      f16x8_t kh, kl;
+      __builtin_memcpy(&kh, kt + x * 1024, 16);
+      __builtin_memcpy(&kl, kt + kPart + x * 1024, 16);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kl, qh[x], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, ql[x], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, qh[x], s, 0, 0, 0);
+    }
+    if (t * kSplitKeys + kSplitKeys - 1 > pos_lo) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vt[8 * (i / 4) + 4 * h + i % 4][32 * d + n], s[i], o[d], 0, 0, 0);
+        if (t * kSplitKeys + 8 * (i / 4) + 4 * h + i % 4 > pos) s[i] = -INFINITY;
     }
-    if (t + 1 < n_tiles) put((t + 1) & 1);
+    const float f = fmaxf(ldexp_f32(kScale * kLog2e, -(eq + ex.x)), 0x1p-120f);  // (0 times -inf is none)
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    top = fmaxf(top, swap32(top)) * f;
+    if (__any(top > m) || ex.y < E) {
+      const float m1 = fmaxf(m, top);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m1);
+      m = m1;
+      l *= keep;
+      const int E1 = min(E, ex.y);
+      const float turn = E == INT_MAX ? 0.f : ldexp_f32(keep, E1 - E);
+      E = E1;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) o[d] *= turn;
+    }
+    const float shift = 14.f - m, part = ldexp_f32(1.f, E - ex.y);
+    f16x8_t ph[2], pl[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float p = __builtin_amdgcn_exp2f(fmaf(s[i], f, shift));
+      l += p;
+      p *= part;
+      ph[i / 8][i % 8] = (_Float16)p;
+      pl[i / 8][i % 8] = (_Float16)(p - (float)ph[i / 8][i % 8]);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        f16x8_t vh, vl;
+        __builtin_memcpy(&vh, kt + 2 * kPart + (4 * x + d) * 1024, 16);
+        __builtin_memcpy(&vl, kt + 3 * kPart + (4 * x + d) * 1024, 16);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vl, ph[x], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, pl[x], o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph[x], o[d], 0, 0, 0);
+      }
   }
   l += swap32(l);
   const float inv = 1.f / l;
@@ -314,9 +434,12 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a)
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(out + 32 * d + 2 * i + 4 * h) =
-            make_float4(o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv);
+      for (int i = 0; i < 16; i += 4) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = ldexp_f32(o[d][i + j] * inv, -E);
+        *reinterpret_cast<float4*>(out + 32 * d + 2 * i + 4 * h) = make_float4(y[0], y[1], y[2], y[3]);
+      }
   }
 }
 
@@ -326,18 +449,30 @@ bool rows_ok(const void* p, size_t ld, int H, int dtype) {
          ld * (dtype == SAKI_F32 ? 4 : 2) % 16 == 0 && ld <= ((size_t)1 << 40);
 }
 
+// Tiles of float32 parts that all prompts have, at most, and the workspace: the
+// exponents behind the tiles.
+long long split_tiles(int T, int B) { return (long long)T / kSplitKeys + B; }
+
 }  // namespace
 
 extern "C" {
 
+size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv) {
+  if (T < 0 || B < 0 || H_kv <= 0 || (dtype != SAKI_F32 && dtype != SAKI_BF16)) return 0;
+  if (dtype == SAKI_BF16 || T == 0 || B == 0) return 256;
+  return (size_t)split_tiles(T, B) * H_kv * (kSplitTile + sizeof(int2));
+}
+
 int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, int T, int B, int H_q, int H_kv,
-                       int d, size_t ld_q, size_t ld_k, size_t ld_v, const int* cu, void* out, void* stream) {
+                       int d, size_t ld_q, size_t ld_k, size_t ld_v, const int* cu, void* out, void* ws,
+                       size_t ws_bytes, void* stream) {
   if (T < 0 || B < 0 || H_q <= 0 || H_kv <= 0 || H_q % H_kv != 0 || d <= 0) return SAKI_ERR_ARG;
   if (d != kHeadDim || (dtype != SAKI_F32 && dtype != SAKI_BF16)) return SAKI_ERR_UNSUPPORTED;
   // row numbers of a KV head fit an int, a launch's threads 32 bits
   const long long rows = (long long)T * (H_q / H_kv);
   const long long tiles = rows / kRows + B;
-  if (rows > INT_MAX / 2 || B > INT_MAX / 2 || tiles * H_kv > (1 << 23)) return SAKI_ERR_UNSUPPORTED;
+  if (rows > INT_MAX / 2 || B > INT_MAX / 2 || tiles * H_kv > (1 << 23) || split_tiles(T, B) * H_kv > (1 << 23))
+    return SAKI_ERR_UNSUPPORTED;
   if (T == 0 || B == 0) return SAKI_OK;
   if (!cu || !out || reinterpret_cast<uintptr_t>(out) % 16 || !rows_ok(q, ld_q, H_q, dtype) ||
       !rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(v, ld_v, H_kv, dtype))
@@ -345,10 +480,18 @@ int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, i
   const PromptArgs a{q, k, v, ld_q, ld_k, ld_v, cu, B, H_q, H_kv, T, out, (int)tiles};
   const dim3 grid((unsigned)(tiles * H_kv));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dtype == SAKI_F32)
-    hipLaunchKernelGGL(prompt_attend_f32_kernel, grid, dim3(256), 0, s, a);
-  else
+  if (dtype == SAKI_BF16) {
     hipLaunchKernelGGL(prompt_attend_kernel, grid, dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? SAKI_OK : SAKI_ERR_HIP;
+  }
+  if (!ws || ws_bytes < saki_attend_prompt_workspace_bytes(dtype, T, B, H_kv) || reinterpret_cast<uintptr_t>(ws) % 16)
+    return SAKI_ERR_WORKSPACE;
+  const long long n = split_tiles(T, B) * H_kv;
+  uint8_t* parts = (uint8_t*)ws;
+  int2* exps = (int2*)(parts + (size_t)n * kSplitTile);
+  hipLaunchKernelGGL(prompt_split_kernel, dim3((unsigned)n), dim3(256), 0, s, a, parts, exps);
+  if (hipGetLastError() != hipSuccess) return SAKI_ERR_HIP;
+  hipLaunchKernelGGL(prompt_attend_f32_kernel, grid, dim3(256), 0, s, a, (const uint8_t*)parts, (const int2*)exps);
   return hipGetLastError() == hipSuccess ? SAKI_OK : SAKI_ERR_HIP;
 }
 

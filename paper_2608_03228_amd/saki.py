@@ -71,7 +71,9 @@ def lib():
         "saki_cache_attend_workspace_bytes": (sz, [ip, ip, ip, ip, ip, ip]),
         "saki_cache_attend": (ip, [vp, ip, ip, ip, ip, ip, ip, vp, vp, vp, ip, vp, ip, vp, vp, ip,
                                    vp, vp, sz, vp]),
-        "saki_attend_prompt": (ip, [vp, vp, vp, ip, ip, ip, ip, ip, ip, sz, sz, sz, vp, vp, vp]),
+        "saki_attend_prompt": (ip, [vp, vp, vp, ip, ip, ip, ip, ip, ip, sz, sz, sz, vp, vp, vp,
+                                    sz, vp]),
+        "saki_attend_prompt_workspace_bytes": (sz, [ip, ip, ip, ip]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -649,9 +651,14 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
     return out
 
 
-def saki_attend_prompt(q, k, v, cu, out=None, stream=None):
+def saki_attend_prompt_workspace_bytes(dtype: str, T, B, H_kv) -> int:
+    return int(lib().saki_attend_prompt_workspace_bytes(_DTYPES[dtype], T, B, H_kv))
+
+
+def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
     """q [T, H_q, d], k, v [T, H_kv, d] (float32 or bfloat16), cu [B + 1] int32:
-    causal attention within each of the packed prompts.  Returns out [T, H_q, d]."""
+    causal attention within each of the packed prompts.  Returns out [T, H_q, d].
+    ws: uint8 workspace (float32 only; allocated if not given)."""
     shape, dt, code = _of_floats(q, 3, "q")
     torch, dev, cur = _current()
     T, H_q, d = shape
@@ -666,8 +673,15 @@ def saki_attend_prompt(q, k, v, cu, out=None, stream=None):
     cp = _array(cu, torch.int32, (n,), dev, "cu")
     if out is None:
         out = _new(stream, shape, dt, q.device)
+    wp, wn = None, 0
+    if ws is None and code == F32:
+        need = lib().saki_attend_prompt_workspace_bytes(F32, T, n - 1, H_kv)
+        ws = _new(stream, max(need, 1), torch.uint8, q.device)
+    if ws is not None:
+        wn = ws.numel()
+        wp = _array(ws, torch.uint8, (wn,), dev, "ws")
     st = lib().saki_attend_prompt(qp, kp, vp_, code, T, n - 1, H_q, H_kv, d, ldq, ldk, ldv, cp,
-                                  _array(out, dt, shape, dev, "out"),
+                                  _array(out, dt, shape, dev, "out"), wp, wn,
                                   cur if stream is None else stream.cuda_stream)
     if st:
         _check("saki_attend_prompt", st)

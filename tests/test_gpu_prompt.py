@@ -1,10 +1,12 @@
 """GPU parity of saki_attend_prompt against the float64 oracle.
 
 Tolerances, before any run.  u = 2^-24, b = 2^-8 (half a bf16 step).
-  scores     128 exact products summed in float32, scaled, and the exponent with
-             its argument: 140 u S + 4 u, S = the row's largest sum of |q_e k_e| /
+  scores     128 products, exact (bf16) or to 2^-21 = 8 u (float32: two fp16 parts
+             an element), summed in float32, scaled, and the exponent with its
+             argument: 140 u S + 4 u, S = the row's largest sum of |q_e k_e| /
              sqrt(d); softmax turns a score error e into 2 e of sum p |v|
-  sums       (N / 32 + 64) u of sum p |v| (a tile, then tile by tile)
+  sums       (N / 32 + 64) u of sum p |v| (a tile, then tile by tile; float32
+             weights and values to 8 u)
   bf16       weights rounded once before they meet the values: b of sum p |v|;
              the output's rounding: b of the output
 """
@@ -177,3 +179,34 @@ def test_prompt_then_decode_steps():
             assert np.all(np.abs(got[b] - want) <= bound)
             # and on the whole much nearer: independent roundings average out
             assert np.linalg.norm(got[b] - want) <= 0.15 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("what", ["keys", "values", "queries", "zeros"])
+def test_attend_prompt_f32_of_very_different_sizes(what):
+    """Elements whose size changes by many powers of two from tile to tile (and
+    tiles of zeros): each output against its own row's bound."""
+    T = 230
+    q, k, v = make(T, 4, 2, "f32", 11)
+    g = 2.0 ** np.repeat(np.array([0, 30, -30, 5, -60, 12, 0, -3]), 32)[:T, None, None]
+    if what == "keys":
+        k, q = rounded(k / np.maximum(g, 1), "f32"), q
+    elif what == "values":
+        v = rounded(v * g, "f32")
+    elif what == "queries":
+        q = rounded(q * np.minimum(g, 8), "f32")
+    else:
+        v[:70] = 0
+        k[64:128] = 0
+        q[5] = 0
+        q[100] *= 2.0 ** -100
+    cu = np.array([0, T])
+    out = S.saki_attend_prompt(dev(q), dev(k), dev(v), ints(cu))
+    # two fp16 parts: 2^-21 of a product and 2^-38 of a tile's largest element more
+    want, mass, size = O.prompt_attend(q, k, v, cu)
+    score = ((140 * U + 2.0 ** -21) * size + 4 * U)[..., None]
+    top = np.maximum.accumulate(np.abs(v).max(-1), 0).repeat(2, 1)[..., None]
+    nxt = np.pad(np.abs(v).max(-1), ((0, 31), (0, 0)))
+    nxt = np.stack([nxt[i:i + T] for i in range(32)]).max(0).repeat(2, 1)[..., None]  # a tile's later values
+    bound = (2 * score + (T / 32 + 64) * U + 2.0 ** -21) * mass + 2.0 ** -37 * T * np.maximum(top, nxt) + U * np.abs(want)
+    err = np.abs(host(out) - want)
+    assert np.all(err <= bound), np.max(err / bound)

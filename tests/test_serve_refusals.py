@@ -96,7 +96,7 @@ def test_cache_attend_workspace():
     assert f(1, 4, 1, 1, 1, 65) == 0
 
 
-PROMPT = "q k v dtype T B H_q H_kv d ld_q ld_k ld_v cu out stream".split()
+PROMPT = "q k v dtype T B H_q H_kv d ld_q ld_k ld_v cu out ws ws_bytes stream".split()
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -104,10 +104,19 @@ PROMPT = "q k v dtype T B H_q H_kv d ld_q ld_k ld_v cu out stream".split()
     (dict(d=0), ARG), (dict(d=64), UNSUP), (dict(dtype=2), UNSUP), (dict(T=1 << 30), UNSUP),
     (dict(B=1 << 30), UNSUP), (dict(q=None), ARG), (dict(k=ODD), ARG), (dict(v=None), ARG), (dict(out=None), ARG),
     (dict(out=ODD), ARG), (dict(cu=None), ARG), (dict(ld_q=511), ARG), (dict(ld_k=128), ARG), (dict(ld_v=260), ARG),
+    (dict(ws=None, dtype=0), WS), (dict(ws_bytes=1000, dtype=0), WS), (dict(ws=ODD, dtype=0), WS),
 ])
 def test_attend_prompt(lib, kw, status):
-    good = [P, P, P, 1, 5, 2, 4, 2, 128, 512, 256, 256, P, P, None]
+    good = [P, P, P, 1, 5, 2, 4, 2, 128, 512, 256, 256, P, P, P, 1 << 30, None]
     assert change(lib.saki_attend_prompt, good, PROMPT, **kw) == status
+
+
+def test_attend_prompt_workspace():
+    f = S.saki_attend_prompt_workspace_bytes
+    assert f("bf16", 1 << 20, 9, 8) == 256 and f("f32", 0, 1, 8) == 256
+    # at least the parts of every token's keys and values, at most two tiles a prompt more
+    assert 4 * 2 * 1000 * 3 * 128 <= f("f32", 1000, 5, 3) <= 4 * 2 * (1000 + 64 * 5 + 32) * 3 * 128
+    assert f("f32", -1, 1, 1) == f("f32", 1, -1, 1) == f("f32", 1, 1, 0) == f("fp8", 1, 1, 1) == 0
 
 
 def test_binding_refuses_host_tensors():
