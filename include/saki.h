@@ -467,7 +467,8 @@ size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv);
  * common power of two for 32 tokens (or one query): 22 bits of each, products
  * to 2^-21.
  *
- *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v apart
+ *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v
+ *           apart (ld up to 2^22)
  *   cu      device int [B + 1], ascending: prompt b is tokens [cu[b], cu[b+1])
  *   out     device [T, H_q, d], dense; tokens of no prompt are left as they were
  *   ws      device workspace of saki_attend_prompt_workspace_bytes(...), 16-byte

@@ -82,7 +82,10 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
 __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
-  __shared__ alignas(1024) uint8_t lds[2][2][kKeys * kHeadDim * 2];  // [buffer][keys, values]
+  // two arrays, and the loop below unrolled over them: a read of one is then
+  // known not to meet the loads into the other, and does not wait for them
+  constexpr int kTileBytes = kKeys * kHeadDim * 2;
+  __shared__ alignas(1024) uint8_t lds_a[2 * kTileBytes], lds_b[2 * kTileBytes];  // keys, values
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
   const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv));
@@ -108,16 +111,26 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
   // to place c ^ (r % 16) (keys), c ^ (r % 4 * 4) (values)
   const __bf16* kp = (const __bf16*)a.k + (size_t)blk.start * a.ld_k + (size_t)hk * kHeadDim;
   const __bf16* vp = (const __bf16*)a.v + (size_t)blk.start * a.ld_v + (size_t)hk * kHeadDim;
-  auto stage = [&](int t, int buf) {
+  uint32_t k_off[4], v_off[4];  // bytes from a tile's first key row; the same for every whole tile
+  auto offsets = [&](int last) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int r = 16 * wave + 4 * u + lane / 16;
-      const int tok = min(t * kKeys + r, blk.len - 1);
-      const int ck = (lane % 16) ^ (r % 16), cv = (lane % 16) ^ (r % 4 * 4);
-      __builtin_amdgcn_global_load_lds((global_void*)(kp + (size_t)tok * a.ld_k + ck * 8),
-                                       (lds_void*)(lds[buf][0] + (16 * wave + 4 * u) * 256), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_void*)(vp + (size_t)tok * a.ld_v + cv * 8),
-                                       (lds_void*)(lds[buf][1] + (16 * wave + 4 * u) * 256), 16, 0, 0);
+      const int r = 16 * wave + 4 * u + lane / 16, at = min(r, last);
+      k_off[u] = (uint32_t)at * (uint32_t)(2 * a.ld_k) + ((lane % 16) ^ (r % 16)) * 16;
+      v_off[u] = (uint32_t)at * (uint32_t)(2 * a.ld_v) + ((lane % 16) ^ (r % 4 * 4)) * 16;
+    }
+  };
+  offsets(kKeys - 1);
+  auto stage = [&](int t, uint8_t* to) __attribute__((always_inline)) {
+    if ((t + 1) * kKeys > blk.len) offsets(blk.len - 1 - t * kKeys);  // (the last tile: past the prompt, its last key)
+    const uint8_t* kt = (const uint8_t*)(kp + (size_t)t * kKeys * a.ld_k);
+    const uint8_t* vt = (const uint8_t*)(vp + (size_t)t * kKeys * a.ld_v);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      __builtin_amdgcn_global_load_lds((global_void*)(kt + k_off[u]), (lds_void*)(to + (16 * wave + 4 * u) * 256), 16,
+                                       0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)(vt + v_off[u]),
+                                       (lds_void*)(to + kTileBytes + (16 * wave + 4 * u) * 256), 16, 0, 0);
     }
   };
 
@@ -131,13 +144,12 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
   const int vs = lane % 16, vg = lane / 16;
   const int v_lane = (4 * (vg / 2) + vs / 4) * 256 + 32 * (vg % 2) + 8 * (vs % 4);
 
-  stage(0, 0);
-  for (int t = 0; t < n_tiles; ++t) {
+  auto tile = [&](int t, const uint8_t* kt, uint8_t* next) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile t
     __syncthreads();
-    if (t + 1 < n_tiles) stage(t + 1, (t + 1) & 1);
-    if (t * kKeys > pos_hi) continue;
-    const uint8_t *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+    if (t + 1 < n_tiles) stage(t + 1, next);
+    if (t * kKeys > pos_hi) return;
+    const uint8_t* vt = kt + kTileBytes;
     f32x16_t s[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -198,6 +210,11 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[d], 0, 0, 0);
       }
     }
+  };
+  stage(0, lds_a);
+  for (int t = 0; t < n_tiles; t += 2) {
+    tile(t, lds_a, lds_b);
+    if (t + 1 < n_tiles) tile(t + 1, lds_b, lds_a);
   }
   l += swap32(l);
   const float inv = 1.f / l;
@@ -317,7 +334,7 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
 
 __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
                                                                    const int2* __restrict__ exps) {
-  __shared__ alignas(1024) uint8_t lds[2][kSplitTile];
+  __shared__ alignas(1024) uint8_t lds_a[kSplitTile], lds_b[kSplitTile];
   constexpr int kPart = kSplitTile / 4;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
@@ -347,11 +364,11 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
   const int pos_hi = (blk.row0 + min(wave * 32 + 31, n_rows - 1)) / G;
   const int n_tiles = (blk.row0 + n_rows - 1) / G / kSplitKeys + 1;
   const size_t tile0 = ((size_t)(blk.start / kSplitKeys + blk.b)) * a.H_kv + hk;
-  auto stage = [&](int t, int buf) {
+  auto stage = [&](int t, uint8_t* to) {
     const uint8_t* p = ws + (tile0 + (size_t)t * a.H_kv) * kSplitTile + wave * 8192 + lane * 16;
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      __builtin_amdgcn_global_load_lds((global_void*)(p + u * 1024), (lds_void*)(lds[buf] + wave * 8192 + u * 1024), 16,
+      __builtin_amdgcn_global_load_lds((global_void*)(p + u * 1024), (lds_void*)(to + wave * 8192 + u * 1024), 16,
                                        0, 0);
   };
 
@@ -364,14 +381,13 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
   // of values times 2^E, E the least exponent of the tiles so far)
   float m = -INFINITY, l = 0.f;
   int E = INT_MAX;
-  stage(0, 0);
-  for (int t = 0; t < n_tiles; ++t) {
+  auto tile = [&](int t, const uint8_t* kt, uint8_t* next) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile t
     __syncthreads();
-    if (t + 1 < n_tiles) stage(t + 1, (t + 1) & 1);
-    if (t * kSplitKeys > pos_hi) continue;
+    if (t + 1 < n_tiles) stage(t + 1, next);
+    if (t * kSplitKeys > pos_hi) return;
     const int2 ex = exps[tile0 + (size_t)t * a.H_kv];
-    const uint8_t* kt = lds[t & 1] + lane * 16;
+    kt += lane * 16;
     f32x16_t s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
@@ -426,6 +442,11 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, pl[x], o[d], 0, 0, 0);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph[x], o[d], 0, 0, 0);
       }
+  };
+  stage(0, lds_a);
+  for (int t = 0; t < n_tiles; t += 2) {
+    tile(t, lds_a, lds_b);
+    if (t + 1 < n_tiles) tile(t + 1, lds_b, lds_a);
   }
   l += swap32(l);
   const float inv = 1.f / l;
@@ -446,8 +467,10 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
 // Token rows of H heads at `p`, ld elements apart: what the 16-byte accesses need.
 bool rows_ok(const void* p, size_t ld, int H, int dtype) {
   return p && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld >= (size_t)H * kHeadDim &&
-         ld * (dtype == SAKI_F32 ? 4 : 2) % 16 == 0 && ld <= ((size_t)1 << 40);
+         ld * (dtype == SAKI_F32 ? 4 : 2) % 16 == 0;
 }
+
+constexpr size_t kMaxLd = 1 << 22;  // a tile's byte offsets fit 32 bits
 
 // Tiles of float32 parts that all prompts have, at most, and the workspace: the
 // exponents behind the tiles.
@@ -477,6 +500,7 @@ int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, i
   if (!cu || !out || reinterpret_cast<uintptr_t>(out) % 16 || !rows_ok(q, ld_q, H_q, dtype) ||
       !rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(v, ld_v, H_kv, dtype))
     return SAKI_ERR_ARG;
+  if (ld_q > kMaxLd || ld_k > kMaxLd || ld_v > kMaxLd) return SAKI_ERR_UNSUPPORTED;
   const PromptArgs a{q, k, v, ld_q, ld_k, ld_v, cu, B, H_q, H_kv, T, out, (int)tiles};
   const dim3 grid((unsigned)(tiles * H_kv));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

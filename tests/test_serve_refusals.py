@@ -103,7 +103,7 @@ PROMPT = "q k v dtype T B H_q H_kv d ld_q ld_k ld_v cu out ws ws_bytes stream".s
     (dict(T=0), 0), (dict(B=0), 0), (dict(T=-1), ARG), (dict(B=-1), ARG), (dict(H_q=3), ARG), (dict(H_kv=0), ARG),
     (dict(d=0), ARG), (dict(d=64), UNSUP), (dict(dtype=2), UNSUP), (dict(T=1 << 30), UNSUP),
     (dict(B=1 << 30), UNSUP), (dict(q=None), ARG), (dict(k=ODD), ARG), (dict(v=None), ARG), (dict(out=None), ARG),
-    (dict(out=ODD), ARG), (dict(cu=None), ARG), (dict(ld_q=511), ARG), (dict(ld_k=128), ARG), (dict(ld_v=260), ARG),
+    (dict(out=ODD), ARG), (dict(cu=None), ARG), (dict(ld_q=511), ARG), (dict(ld_k=128), ARG), (dict(ld_v=260), ARG), (dict(ld_q=(1 << 22) + 8), UNSUP),
     (dict(ws=None, dtype=0), WS), (dict(ws_bytes=1000, dtype=0), WS), (dict(ws=ODD, dtype=0), WS),
 ])
 def test_attend_prompt(lib, kw, status):
