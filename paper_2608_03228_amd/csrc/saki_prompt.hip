@@ -28,6 +28,11 @@ constexpr float kScale = 0.08838834764831845f;  // 1 / sqrt(d)
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kRows = 128;    // query rows of a work-group (32 a wave)
 constexpr int kKeys = 64;     // keys of a tile
+// A row's sums are scaled down only once a score passes the maximum they go by
+// by this many powers of two: a weight may be 2^kSlack, which neither bf16 nor
+// the sums mind, and most tiles that bring a new maximum to one of a wave's 32
+// rows cost no pass over its sums.
+constexpr float kSlack = 8.f;
 
 struct PromptArgs {
   const void *q, *k, *v;
@@ -175,7 +180,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
     top = fmaxf(top, swap32(top));
-    if (__any(top > m)) {
+    if (__any(top > m + kSlack / (kScale * kLog2e))) {
       const float m1 = fmaxf(m, top);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m1) * (kScale * kLog2e));
       m = m1;
@@ -377,8 +382,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-  // m: the running maximum in powers of two; o and l hold sums of 2^14 p (and o
-  // of values times 2^E, E the least exponent of the tiles so far)
+  // m: the running maximum in powers of two; o and l hold sums of 2^6 p (so that
+  // fp16 holds them, 2^(6 + kSlack) at most), and o of values times 2^E, E the
+  // least exponent of the tiles so far
   float m = -INFINITY, l = 0.f;
   int E = INT_MAX;
   auto tile = [&](int t, const uint8_t* kt, uint8_t* next) __attribute__((always_inline)) {
@@ -410,7 +416,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = fmaxf(top, swap32(top)) * f;
-    if (__any(top > m) || ex.y < E) {
+    if (__any(top > m + kSlack) || ex.y < E) {
       const float m1 = fmaxf(m, top);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m1);
       m = m1;
@@ -421,7 +427,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[d] *= turn;
     }
-    const float shift = 14.f - m, part = ldexp_f32(1.f, E - ex.y);
+    const float shift = 6.f - m, part = ldexp_f32(1.f, E - ex.y);
     f16x8_t ph[2], pl[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
