@@ -43,29 +43,30 @@ struct PromptArgs {
   int tiles;  // row blocks of all prompts, at most
 };
 
-// Row block `x` of the packed prompts.  The rows of one KV head are (token,
-// query head of its group) pairs, token after token; a prompt's blocks of
-// kRows rows start at floor(first row / kRows) + b, which leaves each prompt
-// its own ones (with gaps), so that a block finds its prompt by bisection.
+// Block `x` of `rows` rows of the packed prompts.  The rows of one KV head are
+// (token, one of its G query heads) pairs, token after token; a prompt's blocks
+// start at floor(first row / rows) + b, which leaves each prompt its own ones
+// (with gaps), so that a block finds its prompt by a search of the offsets.
 struct Block {
   int b, start, len, row0;  // prompt, its first token and length, first row in it; len = 0: none
 };
-__device__ __forceinline__ Block find_block(const PromptArgs& a, int x) {
-  const int G = a.H_q / a.H_kv;
+__device__ __forceinline__ Block find_block(const PromptArgs& a, int x, int G, int rows) {
   auto at = [&](int b) { return min(max(a.cu[b], 0), a.T); };
-  int lo = 0, hi = a.B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if ((long long)at(mid) * G / kRows + mid <= x)
-      lo = mid;
-    else
-      hi = mid;
+  int lo = 0, n = a.B;  // the prompt is one of lo .. lo + n - 1: a wave tells 64 parts of them apart at once
+  while (n > 1) {
+    const int step = (n + kWave - 1) / kWave, i = (int)(threadIdx.x % kWave) * step;
+    const bool below = i < n && (long long)at(lo + i) * G / rows + lo + i <= x;
+    const uint64_t which = __ballot(below);  // none: the block lies before the first prompt
+    const int part = which ? (63 - __builtin_clzll(which)) * step : 0;
+    n = min(n - part, step);
+    lo += part;
   }
+  lo = __builtin_amdgcn_readfirstlane(lo);
   Block r;
   r.b = lo;
   r.start = at(lo);
   r.len = max(at(lo + 1) - r.start, 0);
-  const long long row0 = (x - ((long long)r.start * G / kRows + lo)) * kRows;
+  const long long row0 = (x - ((long long)r.start * G / rows + lo)) * rows;
   if (row0 < 0 || row0 >= (long long)r.len * G) r.len = 0;
   r.row0 = (int)row0;
   return r;
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
   __shared__ alignas(1024) uint8_t lds_a[2 * kTileBytes], lds_b[2 * kTileBytes];  // keys, values
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
-  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv));
+  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv), G, kRows);
   if (blk.len == 0) return;
   const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kRows);
   const int n = lane % 32, h = lane / 32;
@@ -269,18 +270,9 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
   __shared__ float part[2][4];
   __shared__ float vals[kSplitKeys][kHeadDim + 4];
   const int hk = blockIdx.x % a.H_kv, tile = blockIdx.x / a.H_kv;
-  int lo_b = 0, hi_b = a.B;
-  auto at = [&](int b) { return min(max(a.cu[b], 0), a.T); };
-  while (hi_b - lo_b > 1) {
-    const int mid = (lo_b + hi_b) >> 1;
-    if (at(mid) / kSplitKeys + mid <= tile)
-      lo_b = mid;
-    else
-      hi_b = mid;
-  }
-  const int start = at(lo_b), len = at(lo_b + 1) - start;
-  const int key0 = (tile - (start / kSplitKeys + lo_b)) * kSplitKeys;
-  if (key0 < 0 || key0 >= len) return;
+  const Block blk = find_block(a, tile, 1, kSplitKeys);
+  if (blk.len == 0) return;
+  const int start = blk.start, len = blk.len, key0 = blk.row0;
   const int tid = threadIdx.x, row = tid / 8, c = tid % 8 * 16;
   float k[16], v[16];
   const bool in = key0 + row < len;
@@ -343,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
   constexpr int kPart = kSplitTile / 4;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
-  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv));
+  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv), G, kRows);
   if (blk.len == 0) return;
   const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kRows);
   const int n = lane % 32, h = lane / 32;

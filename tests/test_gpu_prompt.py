@@ -72,6 +72,19 @@ def test_attend_prompt_leaves_other_tokens_and_reads_none(dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attend_prompt_behind_many_other_tokens(dt):
+    """Row blocks that lie before the first prompt, and between the last one and
+    the end, belong to none; more prompts than a search step tells apart."""
+    cu = np.concatenate([[400], 400 + np.cumsum(np.arange(90) % 4)])
+    T = cu[-1] + 333
+    q, k, v = make(T, 4, 2, dt, 12)
+    out = torch.full((T, 4, 128), 7.0, dtype=DT[dt], device=DEV)
+    got = S.saki_attend_prompt(*(dev(x, DT[dt]) for x in (q, k, v)), ints(cu), out=out)
+    got, inside = check(got, q, k, v, cu, dt)
+    assert (got[~inside] == 7).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_attend_prompt_of_a_fused_projection(dt):
     """q, k, v as slices of one [T, H_q + 2 H_kv, d] tensor."""
     H_q, H_kv, cu = 6, 2, np.array([0, 90, 131])
@@ -95,12 +108,18 @@ def test_attend_prompt_rising_and_peaked_scores(dt):
     check(out, q, k, v, np.array([0, T]), dt)
 
 
-def test_attend_prompt_offsets_that_do_not_ascend_stay_in_range():
-    """Such offsets are the caller's mistake: nothing outside the arrays is read
-    or written (what is written is not specified)."""
-    q, k, v = (dev(x) for x in make(100, 4, 2, "f32", 4))
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attend_prompt_offsets_that_do_not_ascend_stay_in_range(dt):
+    """Such offsets are the caller's mistake: what is written to out is not
+    specified, but nothing outside it is."""
+    q, k, v = (dev(x, DT[dt]) for x in make(100, 4, 2, dt, 4))
+    need = S.saki_attend_prompt_workspace_bytes(dt, 100, 2, 2)
     for cu in ([0, 2000000000, 50], [-5, 60, 1000], [90, 10, 95], [2147483647, -2147483648, 7]):
-        assert torch.isfinite(S.saki_attend_prompt(q, k, v, ints(cu), out=torch.zeros_like(q))).all()
+        out = torch.full((300, 4, 128), 7.0, dtype=DT[dt], device=DEV)
+        ws = torch.full((need + 8192,), 9, dtype=torch.uint8, device=DEV)
+        S.saki_attend_prompt(q, k, v, ints(cu), out=out[100:200], ws=ws[4096:4096 + need])
+        assert (out[:100] == 7).all() and (out[200:] == 7).all()
+        assert (ws[:4096] == 9).all() and (ws[4096 + need:] == 9).all()
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
