@@ -36,28 +36,26 @@ __device__ __forceinline__ float xor_f32(float v, int m) {
   return __uint_as_float(xor_shfl_u32(__float_as_uint(v), m));
 }
 
-// Elements [i, i + N) of a float32 or bf16 array as floats; N elements fill
-// 16 bytes (or two or four times that), and i is a multiple of N.
-template <typename T, int N>
-__device__ __forceinline__ void load_elems(const T* p, float* out) {
-  if constexpr (std::is_same_v<T, float>) {
+// The 4 float32 or 8 bf16 elements of 16 bytes as floats.
+template <typename T>
+__device__ __forceinline__ void unpack16(uint4 v, float* out) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int j = 0; j < N; j += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(p + j);
-      out[j] = v.x, out[j + 1] = v.y, out[j + 2] = v.z, out[j + 3] = v.w;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; j += 8) {
-      const uint4 v = *reinterpret_cast<const uint4*>(p + j);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        out[j + 2 * e] = __uint_as_float(w[e] << 16);
-        out[j + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-      }
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (std::is_same_v<T, float>) {
+      out[e] = __uint_as_float(w[e]);
+    } else {
+      out[2 * e] = __uint_as_float(w[e] << 16);
+      out[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
   }
+}
+
+// N elements at p, a 16-byte boundary, as floats.
+template <typename T, int N>
+__device__ __forceinline__ void load_elems(const T* p, float* out) {
+#pragma unroll
+  for (int j = 0; j < N; j += 16 / (int)sizeof(T)) unpack16<T>(*reinterpret_cast<const uint4*>(p + j), out + j);
 }
 
 // Two floats as a pair of bf16, round to nearest even.
@@ -294,17 +292,10 @@ __global__ __launch_bounds__(256) void block_tables_kernel(
 
 // ---------------------------------------------------------------- writing the cache
 
-// 16 floats as 16 E4M3 codes: nearest, ties to the even code.
-__device__ __forceinline__ uint4 encode16(const float* x, float inv) {
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    int v = 0;
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j] * inv, x[4 * j + 1] * inv, v, false);
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2] * inv, x[4 * j + 3] * inv, v, true);
-    w[j] = (uint32_t)v;
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+// Four floats times inv as E4M3 codes: nearest, ties to the even code.
+__device__ __forceinline__ uint32_t encode4(const float* x, float inv) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, lo, true);
 }
 
 __device__ __forceinline__ void decode16(uint4 v, float* x) {
@@ -327,80 +318,164 @@ __device__ __forceinline__ int scale_exponent(float top) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// A run is a stretch of tokens whose slots ascend within one block.  One
-// work-group takes one run of one head, for the keys (z = 0) or the values
-// (z = 1); a run belongs to the window of tokens in which it begins.  The
-// block's scale is the least power of two that covers the run, and, where
-// the block holds tokens before the run, no less than it was; if it grew, the
-// codes before the run are moved to it.  Powers of two make that exact but for
-// codes that become subnormal, and codes times scale exact in bf16.
-// HBM bound on prompts, latency on single tokens.
+// A run is a stretch of tokens whose slots ascend within one block; it belongs
+// to the window of tokens in which it begins.  One wave takes the runs of one
+// window for one head's keys or values and holds a whole run (up to 64 rows of
+// 512 bytes) in registers between the search for its largest element and the
+// rounding, all its loads in flight at once.  The block's scale is the least
+// power of two that covers the run, and, where the block holds tokens before
+// the run, no less than it was; if it grew, the codes before the run are moved
+// to it.  Powers of two make that exact but for codes that become subnormal,
+// and codes times scale exact in bf16.  HBM bound on prompts, latency on single
+// tokens.
 template <typename T>
-__global__ __launch_bounds__(256) void cache_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
-                                                          size_t ld_k, size_t ld_v, int n_tokens, int window,
-                                                          const int* __restrict__ slots, int n_blocks, int H,
-                                                          uint8_t* k_cache, uint8_t* v_cache, float* scales) {
-  __shared__ float part[4];
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int h = blockIdx.y, which = blockIdx.z;
-  const T* src = which ? v : k;
+__global__ __launch_bounds__(256, 2) void cache_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
+                                                             size_t ld_k, size_t ld_v, int n_tokens, int window,
+                                                             const int* __restrict__ slots, int n_blocks, int H,
+                                                             uint8_t* k_cache, uint8_t* v_cache, float* scales) {
+  constexpr int V = 16 / sizeof(T);         // elements a lane loads at once
+  constexpr int kLanes = kHeadDim / V;      // lanes a row
+  constexpr int kStep = kWave / kLanes;     // rows the wave loads at once
+  constexpr int kLoads = kTile / kStep, kGroup = 8;
+  const int lane = threadIdx.x % kWave, unit = blockIdx.y * 4 + threadIdx.x / kWave;
+  if (unit >= 2 * H) return;
+  const int h = unit >> 1, which = unit & 1;
+  const T* src = (which ? v : k) + (size_t)h * kHeadDim;
   const size_t ld = which ? ld_v : ld_k;
-  uint8_t* cache = which ? v_cache : k_cache;
   const int n_slots = n_blocks * kTile;
-  const int t_end = min(n_tokens, ((int)blockIdx.x + 1) * window);
-  for (int t = blockIdx.x * window; t < t_end;) {
-    // slots t - 1 .. t + 63: whether t begins a run, and where the run ends
-    const int s = t + lane < n_tokens ? slots[t + lane] : -1;
-    const int before = t > 0 && lane == 0 ? slots[t - 1] : -1;
-    const int s0 = __builtin_amdgcn_readfirstlane(s), sb = __builtin_amdgcn_readfirstlane(before);
-    if (s0 < 0 || s0 >= n_slots || (sb >= 0 && sb < s0 && sb / kTile == s0 / kTile)) {
-      ++t;
-      continue;
+  const int t0 = blockIdx.x * window;
+  // tokens t0 - 1 .. t0 + 127: where runs begin and where they go on
+  const int s0 = t0 + lane < n_tokens ? slots[t0 + lane] : -1;
+  const int s1 = t0 + kWave + lane < n_tokens ? slots[t0 + kWave + lane] : -1;
+  int p0 = __shfl_up(s0, 1), p1 = __shfl_up(s1, 1);
+  if (lane == 0) p0 = t0 > 0 ? slots[t0 - 1] : -1;
+  const int last0 = __builtin_amdgcn_readlane(s0, kWave - 1);
+  if (lane == 0) p1 = last0;
+  auto goes_on = [&](int s, int p) { return p >= 0 && p < s && s < n_slots && s / kTile == p / kTile; };
+  const bool on0 = goes_on(s0, p0);
+  const uint64_t on_a = __ballot(on0), on_b = __ballot(goes_on(s1, p1));
+  uint64_t begins = __ballot(lane < window && s0 >= 0 && s0 < n_slots && !on0);
+  const uint64_t ones = begins & ~((on_a >> 1) | (on_b << (kWave - 1)));
+  const int row = lane / kLanes, col = lane % kLanes * V;
+  uint8_t* const cache = which ? v_cache : k_cache;
+  // moves the codes before slot `first` of a block to a grown scale
+  auto move = [&](uint8_t* block, int first, float ratio) {
+    for (int i = lane / 8; i < first; i += 8) {
+      uint4* o = reinterpret_cast<uint4*>(block + i * kHeadDim + lane % 8 * 16);
+      float y[16];
+      decode16(*o, y);
+      *o = make_uint4(encode4(y, ratio), encode4(y + 4, ratio), encode4(y + 8, ratio), encode4(y + 12, ratio));
     }
-    const int prev = __shfl_up(s, 1);
-    const uint64_t stop = __ballot(lane > 0 && !(s > prev && s / kTile == s0 / kTile));
-    const int n = stop ? __builtin_ctzll(stop) : kTile;
-    const int blk = s0 / kTile, first = s0 % kTile;
-    uint8_t* out = cache + ((size_t)blk * H + h) * kBlockBytes;
-    float* scale = scales + ((size_t)blk * H + h) * 2 + which;
-    const float old = first ? *scale : 0.f;
-    const int row = tid / 8, col = tid % 8 * 16;
-    float x[2][16], top = 0.f;
-    int at[2];
+  };
+
+  // runs of one token (decode steps), a row of lanes each, up to 32 at once
+  constexpr int kBatch = kStep * kGroup;
+  for (int b = 0; b < window; b += kBatch) {
+    const uint64_t now_ones = ones >> b & ((1ull << kBatch) - 1);
+    if (!now_ones) continue;
+    uint4 x[kGroup];
+    int slot[kGroup];
+    float old[kGroup];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int i = row + 32 * u;
-      at[u] = __shfl(s, i) % kTile;
-      if (i < n) {
-        load_elems<T, 16>(src + (size_t)(t + i) * ld + (size_t)h * kHeadDim + col, x[u]);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[u][e]));
+    for (int u = 0; u < kGroup; ++u) {
+      slot[u] = -1;
+      x[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (now_ones >> (u * kStep) & ((1u << kStep) - 1)) {
+        const int at = u * kStep + row, sl = __shfl(s0, b + at);
+        if (now_ones >> at & 1) {
+          slot[u] = sl;
+          x[u] = *reinterpret_cast<const uint4*>(src + (size_t)(t0 + b + at) * ld + col);
+          old[u] = scales[((size_t)(sl / kTile) * H + h) * 2 + which];
+        }
       }
     }
 #pragma unroll
+    for (int u = 0; u < kGroup; ++u)
+      if (now_ones >> (u * kStep) & ((1u << kStep) - 1)) {
+        float y[V], top = 0.f, ratio = 0.f;
+        unpack16<T>(x[u], y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(y[e]));
+#pragma unroll
+        for (int m = 1; m < kLanes; m <<= 1) top = fmaxf(top, xor_f32(top, m));
+        const int blk = slot[u] / kTile, first = slot[u] % kTile;
+        bool grew = false;
+        if (slot[u] >= 0) {
+          const int e = scale_exponent(top);
+          grew = first && !(old[u] >= pow2(e));
+          const bool keeps = first && !grew;
+          const float inv = keeps ? 1.f / old[u] : pow2(-e);
+          ratio = old[u] * inv;
+          uint32_t w[V / 4];
+#pragma unroll
+          for (int j = 0; j < V / 4; ++j) w[j] = encode4(y + 4 * j, inv);
+          __builtin_memcpy(cache + ((size_t)blk * H + h) * kBlockBytes + first * kHeadDim + col, w, V);
+          if (col == 0 && !keeps) scales[((size_t)blk * H + h) * 2 + which] = pow2(e);
+        }
+        for (uint64_t g = __ballot(grew && col == 0); g; g &= g - 1) {
+          const int l = __builtin_ctzll(g);
+          move(cache + ((size_t)__builtin_amdgcn_readlane(blk, l) * H + h) * kBlockBytes,
+               __builtin_amdgcn_readlane(first, l),
+               __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(ratio), l)));
+        }
+      }
+  }
+
+  for (begins &= ~ones; begins; begins &= begins - 1) {
+    const int at = __builtin_ctzll(begins), t = t0 + at;
+    // the tokens after `at` that go on: at most 63, as a block's slots ascend
+    const uint64_t on = at == kWave - 1 ? on_b : (on_a >> (at + 1)) | (on_b << (kWave - 1 - at));
+    const int n = ~on ? 1 + __builtin_ctzll(~on) : kTile;
+    const int slot = __builtin_amdgcn_readlane(s0, at);
+    const int blk = slot / kTile, first = slot % kTile;
+    uint8_t* out = cache + ((size_t)blk * H + h) * kBlockBytes;
+    float* scale = scales + ((size_t)blk * H + h) * 2 + which;
+    uint4 x[kLoads];
+    float top = 0.f;
+    const T* p = src + (size_t)(t + row) * ld + col;
+#pragma unroll
+    for (int g = 0; g < kLoads; g += kGroup)
+      if (g * kStep < n)
+#pragma unroll
+        for (int u = g; u < g + kGroup; ++u) {
+          x[u] = make_uint4(0u, 0u, 0u, 0u);
+          if (row + u * kStep < n) x[u] = *reinterpret_cast<const uint4*>(p + (size_t)(u * kStep) * ld);
+        }
+    const float old = first ? *scale : 0.f;
+#pragma unroll
+    for (int g = 0; g < kLoads; g += kGroup)
+      if (g * kStep < n)
+#pragma unroll
+        for (int u = g; u < g + kGroup; ++u) {
+          float y[V];
+          unpack16<T>(x[u], y);
+#pragma unroll
+          for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(y[e]));
+        }
+#pragma unroll
     for (int m = 1; m < kWave; m <<= 1) top = fmaxf(top, xor_f32(top, m));
-    __syncthreads();  // the last run's readers are done with `part`
-    if (lane == 0) part[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
     const int e = scale_exponent(top);
     const bool grew = first && !(old >= pow2(e));
     const float now = first && !grew ? old : pow2(e);
     const float inv = first && !grew ? 1.f / now : pow2(-e);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (row + 32 * u < n) *reinterpret_cast<uint4*>(out + at[u] * kHeadDim + col) = encode16(x[u], inv);
-    if (grew) {
-      const float ratio = old * inv;
-      for (int i = row; i < first; i += 32) {
-        uint4* p = reinterpret_cast<uint4*>(out + i * kHeadDim + col);
-        float y[16];
-        decode16(*p, y);
-        *p = encode16(y, ratio);
-      }
-    }
-    if (tid == 0 && (!first || grew)) *scale = now;
-    t += n;
+    for (int g = 0; g < kLoads; g += kGroup)
+      if (g * kStep < n)
+#pragma unroll
+        for (int u = g; u < g + kGroup; ++u) {
+          const int i = row + u * kStep;
+          if (i < n) {
+            const int to = slots[t + i] % kTile;
+            float y[V];
+            unpack16<T>(x[u], y);
+            uint32_t w[V / 4];
+#pragma unroll
+            for (int j = 0; j < V / 4; ++j) w[j] = encode4(y + 4 * j, inv);
+            __builtin_memcpy(out + to * kHeadDim + col, w, V);
+          }
+        }
+    if (grew) move(out, first, old * inv);
+    if (lane == 0 && (!first || grew)) *scale = now;
   }
 }
 
@@ -948,8 +1023,10 @@ int saki_cache_write(const void* k, const void* v, int dtype, int T, int H_kv, i
   if (T == 0) return SAKI_OK;
   if (!slots || !rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(v, ld_v, H_kv, dtype)) return SAKI_ERR_ARG;
   if (n_blocks == 0) return SAKI_OK;  // no slot is within it
-  const int window = T <= 4096 ? 1 : 8;
-  const dim3 grid((T + window - 1) / window, H_kv, 2);
+  // about 4,096 waves, as many as the GPU holds twice; a window is one wave's
+  int window = 1;
+  while (window < kWave && (long long)T * 2 * H_kv > 4096LL * window) window *= 2;
+  const dim3 grid((T + window - 1) / window, (2 * H_kv + 3) / 4);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (dtype == SAKI_F32)
     hipLaunchKernelGGL((cache_write_kernel<float>), grid, dim3(256), 0, s, (const float*)k, (const float*)v, ld_k,
