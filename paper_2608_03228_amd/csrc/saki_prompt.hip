@@ -87,20 +87,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
+template <int KS>
 __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
+  constexpr int kBlockRows = kRows / KS;
   // two arrays, and the loop below unrolled over them: a read of one is then
   // known not to meet the loads into the other, and does not wait for them
   constexpr int kTileBytes = kKeys * kHeadDim * 2;
   __shared__ alignas(1024) uint8_t lds_a[2 * kTileBytes], lds_b[2 * kTileBytes];  // keys, values
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
-  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv), G, kRows);
+  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv), G, kBlockRows);
   if (blk.len == 0) return;
-  const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kRows);
+  const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kBlockRows);
   const int n = lane % 32, h = lane / 32;
 
-  // this lane's query row, its token and head
-  const int row = min(wave * 32 + n, n_rows - 1) + blk.row0;
+  // this wave's 32 rows and its part of a tile's keys; this lane's row, its token and head
+  const int rw = KS == 1 ? wave * 32 : wave % 2 * 32, b0 = KS == 1 ? 0 : wave / 2;
+  const int row = min(rw + n, n_rows - 1) + blk.row0;
   const int pos = row / G;
   const size_t q_at = (size_t)(blk.start + pos) * a.ld_q + (size_t)(hk * G + row % G) * kHeadDim;
   bf16x8_t q[8];
@@ -109,8 +112,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
     const uint4 v = *reinterpret_cast<const uint4*>((const __bf16*)a.q + q_at + 16 * s + 8 * h);
     __builtin_memcpy(&q[s], &v, 16);
   }
-  const int pos_lo = (blk.row0 + min(wave * 32, n_rows - 1)) / G;
-  const int pos_hi = (blk.row0 + min(wave * 32 + 31, n_rows - 1)) / G;
+  const int pos_lo = (blk.row0 + min(rw, n_rows - 1)) / G;
+  const int pos_hi = (blk.row0 + min(rw + 31, n_rows - 1)) / G;
   const int n_tiles = (blk.row0 + n_rows - 1) / G / kKeys + 1;
 
   // staging: a wave's load takes 4 rows of 16 pieces; piece c of key row r goes
@@ -156,30 +159,28 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
     if (t + 1 < n_tiles) stage(t + 1, next);
     if (t * kKeys > pos_hi) return;
     const uint8_t* vt = kt + kTileBytes;
-    f32x16_t s[2];
+    f32x16_t s[2 / KS];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < 2 / KS; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         bf16x8_t kf;
-        __builtin_memcpy(&kf, kt + b * 32 * 256 + (k_lane ^ (x * 32)), 16);
+        __builtin_memcpy(&kf, kt + (b + b0) * 32 * 256 + (k_lane ^ (x * 32)), 16);
         s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x], s[b], 0, 0, 0);
       }
     }
     if (t * kKeys + kKeys - 1 > pos_lo) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2 / KS; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (t * kKeys + 32 * b + 8 * (i / 4) + 4 * h + i % 4 > pos) s[b][i] = -INFINITY;
+          if (t * kKeys + 32 * (b + b0) + 8 * (i / 4) + 4 * h + i % 4 > pos) s[b][i] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
+    for (int i = 1; i < 32 / KS; ++i) top = fmaxf(top, s[i / 16][i % 16]);
     top = fmaxf(top, swap32(top));
     if (__any(top > m + kSlack / (kScale * kLog2e))) {
       const float m1 = fmaxf(m, top);
@@ -189,10 +190,11 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[d] *= keep;
     }
-    const float shift = -m * (kScale * kLog2e);
-    uint32_t p[16];
+    // (a part of the keys may hold none that a row sees)
+    const float shift = KS > 1 && m == -INFINITY ? 0.f : -m * (kScale * kLog2e);
+    uint32_t p[16 / KS];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2 / KS; ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], kScale * kLog2e, shift));
@@ -201,13 +203,13 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
         p[8 * b + i / 2] = pack_bf16(p0, p1);
       }
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {  // 16 keys each
+    for (int x = 0; x < 4 / KS; ++x) {  // 16 keys each
       bf16x8_t pf;
       __builtin_memcpy(&pf, &p[4 * x], 16);
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
-        const uint8_t* at = vt + x * 16 * 256 + (v_lane ^ ((d ^ (vs / 4)) * 64));
+        const uint8_t* at = vt + (x + 2 * b0) * 16 * 256 + (v_lane ^ ((d ^ (vs / 4)) * 64));
         const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds_void*)at);
         const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds_void*)(at + 8 * 256));
         bf16x8_t vf;
@@ -223,8 +225,32 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
     if (t + 1 < n_tiles) tile(t + 1, lds_b, lds_a);
   }
   l += swap32(l);
+  if constexpr (KS == 2) {  // the second waves' sums join the first ones', through the tiles' memory
+    __syncthreads();
+    float* x = (float*)(rw ? lds_b : lds_a);  // [64 sums, maximum and weight][lane]
+    static_assert(2 * kTileBytes >= 64 * kWave * 4);
+    __shared__ float ml[2][2][kWave];
+    if (b0 == 1) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(16 * d + i) * kWave + lane] = o[d][i];
+      ml[rw / 32][0][lane] = m;
+      ml[rw / 32][1][lane] = l;
+    }
+    __syncthreads();
+    if (b0 == 1) return;
+    const float m2 = ml[rw / 32][0][lane], l2 = ml[rw / 32][1][lane], m1 = fmaxf(m, m2);
+    const float e1 = __builtin_amdgcn_exp2f((m - m1) * (kScale * kLog2e));
+    const float e2 = __builtin_amdgcn_exp2f((m2 - m1) * (kScale * kLog2e));
+    l = l * e1 + l2 * e2;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * e1 + x[(16 * d + i) * kWave + lane] * e2;
+  }
   const float inv = 1.f / l;
-  if (wave * 32 + n < n_rows) {
+  if (rw + n < n_rows) {
     __bf16* out = (__bf16*)a.out + ((size_t)(blk.start + pos) * a.H_q + hk * G + row % G) * kHeadDim;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -329,17 +355,20 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
   }
 }
 
+template <int KS>
 __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
                                                                    const int2* __restrict__ exps) {
-  __shared__ alignas(1024) uint8_t lds_a[kSplitTile], lds_b[kSplitTile];
-  constexpr int kPart = kSplitTile / 4;
+  __shared__ alignas(1024) uint8_t lds_a[KS * kSplitTile], lds_b[KS * kSplitTile];
+  constexpr int kPart = kSplitTile / 4, kBlockRows = kRows / KS;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
-  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv), G, kRows);
+  const Block blk = find_block(a, a.tiles - 1 - (int)(blockIdx.x / a.H_kv), G, kBlockRows);
   if (blk.len == 0) return;
-  const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kRows);
+  const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kBlockRows);
   const int n = lane % 32, h = lane / 32;
-  const int row = min(wave * 32 + n, n_rows - 1) + blk.row0;
+  // this wave's 32 rows and which of a step's KS tiles it takes
+  const int rw = KS == 1 ? wave * 32 : wave % 2 * 32, b0 = KS == 1 ? 0 : wave / 2;
+  const int row = min(rw + n, n_rows - 1) + blk.row0;
   const int pos = row / G;
   const float* qp = (const float*)a.q + (size_t)(blk.start + pos) * a.ld_q + (size_t)(hk * G + row % G) * kHeadDim;
   f16x8_t qh[8], ql[8];
@@ -357,17 +386,22 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
 #pragma unroll
     for (int s = 0; s < 8; ++s) split_f16(x + 8 * s, eq, &qh[s], &ql[s]);
   }
-  const int pos_lo = (blk.row0 + min(wave * 32, n_rows - 1)) / G;
-  const int pos_hi = (blk.row0 + min(wave * 32 + 31, n_rows - 1)) / G;
+  const int pos_lo = (blk.row0 + min(rw, n_rows - 1)) / G;
+  const int pos_hi = (blk.row0 + min(rw + 31, n_rows - 1)) / G;
   const int n_tiles = (blk.row0 + n_rows - 1) / G / kSplitKeys + 1;
   const size_t tile0 = ((size_t)(blk.start / kSplitKeys + blk.b)) * a.H_kv + hk;
-  auto stage = [&](int t, uint8_t* to) {
-    const uint8_t* p = ws + (tile0 + (size_t)t * a.H_kv) * kSplitTile + wave * 8192 + lane * 16;
+  auto stage = [&](int step, uint8_t* to) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      __builtin_amdgcn_global_load_lds((global_void*)(p + u * 1024), (lds_void*)(to + wave * 8192 + u * 1024), 16,
-                                       0, 0);
+    for (int j = 0; j < KS; ++j) {
+      const int t = min(step * KS + j, n_tiles - 1);
+      const uint8_t* p = ws + (tile0 + (size_t)t * a.H_kv) * kSplitTile + wave * 8192 + lane * 16;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        __builtin_amdgcn_global_load_lds((global_void*)(p + u * 1024),
+                                         (lds_void*)(to + j * kSplitTile + wave * 8192 + u * 1024), 16, 0, 0);
+    }
   };
+  const int n_steps = (n_tiles + KS - 1) / KS;
 
   f32x16_t o[4];
 #pragma unroll
@@ -379,11 +413,13 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
   // least exponent of the tiles so far
   float m = -INFINITY, l = 0.f;
   int E = INT_MAX;
-  auto tile = [&](int t, const uint8_t* kt, uint8_t* next) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of tile t
+  auto tile = [&](int step, const uint8_t* kt, uint8_t* next) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the step's tiles
     __syncthreads();
-    if (t + 1 < n_tiles) stage(t + 1, next);
+    if (step + 1 < n_steps) stage(step + 1, next);
+    const int t = step * KS + b0;
     if (t * kSplitKeys > pos_hi) return;
+    kt += b0 * kSplitTile;
     const int2 ex = exps[tile0 + (size_t)t * a.H_kv];
     kt += lane * 16;
     f32x16_t s;
@@ -419,7 +455,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[d] *= turn;
     }
-    const float shift = 6.f - m, part = ldexp_f32(1.f, E - ex.y);
+    const float shift = KS > 1 && m == -INFINITY ? 0.f : 6.f - m, part = ldexp_f32(1.f, E - ex.y);
     f16x8_t ph[2], pl[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -442,13 +478,41 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
       }
   };
   stage(0, lds_a);
-  for (int t = 0; t < n_tiles; t += 2) {
-    tile(t, lds_a, lds_b);
-    if (t + 1 < n_tiles) tile(t + 1, lds_b, lds_a);
+  for (int step = 0; step < n_steps; step += 2) {
+    tile(step, lds_a, lds_b);
+    if (step + 1 < n_steps) tile(step + 1, lds_b, lds_a);
   }
   l += swap32(l);
+  if constexpr (KS == 2) {  // the second waves' sums join the first ones', through the tiles' memory
+    __syncthreads();
+    float* x = (float*)(rw ? lds_b : lds_a);  // [64 sums][lane]
+    __shared__ float ml[2][2][kWave];
+    __shared__ int es[2];
+    if (b0 == 1) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(16 * d + i) * kWave + lane] = o[d][i];
+      ml[rw / 32][0][lane] = m;
+      ml[rw / 32][1][lane] = l;
+      es[rw / 32] = E;
+    }
+    __syncthreads();
+    if (b0 == 1) return;
+    const float m2 = ml[rw / 32][0][lane], l2 = ml[rw / 32][1][lane], m1 = fmaxf(m, m2);
+    const int E2 = es[rw / 32], E1 = min(E, E2);  // (the first waves have a tile each)
+    float e1 = __builtin_amdgcn_exp2f(m - m1), e2 = __builtin_amdgcn_exp2f(m2 - m1);
+    l = l * e1 + l2 * e2;
+    e1 = ldexp_f32(e1, E1 - E);
+    e2 = E2 == INT_MAX ? 0.f : ldexp_f32(e2, E1 - E2);
+    E = E1;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * e1 + x[(16 * d + i) * kWave + lane] * e2;
+  }
   const float inv = 1.f / l;
-  if (wave * 32 + n < n_rows) {
+  if (rw + n < n_rows) {
     float* out = (float*)a.out + ((size_t)(blk.start + pos) * a.H_q + hk * G + row % G) * kHeadDim;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -466,6 +530,26 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a,
 bool rows_ok(const void* p, size_t ld, int H, int dtype) {
   return p && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld >= (size_t)H * kHeadDim &&
          ld * (dtype == SAKI_F32 ? 4 : 2) % 16 == 0;
+}
+
+// Whether blocks of half the rows, whose waves take a tile's keys in two parts,
+// are the better ones: a block's time halves, but not the work before and after
+// its tiles, so that it needs CUs without a block of their own and keys to part.
+// us, whole / halved, prompts x tokens of H_q / H_kv heads:
+//                        blocks    bf16           float32
+//   4 x 64, 32 / 8           96     8.0 / 7.7     15.4 / 13.7
+//   6 x 128, 32 / 8         240     8.7 / 9.3     20.9 / 25.0
+//   2 x 400, 32 / 8         216    13.0 / 13.0    33.2 / 28.7
+//   4 x 400, 32 / 8         432    18.2 / 21.2    42.6 / 51.9
+//   3000, 8 / 8             192    58.2 / 42.4   165.6 / 95.3
+//   1200, 28 / 4            264    28.8 / 23.2    69.7 / 62.1
+//   4 x 300, 28 / 4         276    12.8 / 13.2    29.9 / 35.6
+//   3 x 1000, 12 / 1        284    25.9 / 22.5    62.0 / 65.1
+//   6000, 8 / 8             376   122.2 / 98.0   336.8 / 304.5
+//   6 x 1024, 8 / 8         432    30.0 / 32.2    86.5 / 92.1
+bool halves_better(long long blocks, int T, int B) {
+  const int keys = T / B;  // of a prompt, on average
+  return blocks <= (keys >= 1000 ? 384 : keys >= 256 ? 224 : 128);
 }
 
 constexpr size_t kMaxLd = 1 << 22;  // a tile's byte offsets fit 32 bits
@@ -491,19 +575,24 @@ int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, i
   if (d != kHeadDim || (dtype != SAKI_F32 && dtype != SAKI_BF16)) return SAKI_ERR_UNSUPPORTED;
   // row numbers of a KV head fit an int, a launch's threads 32 bits
   const long long rows = (long long)T * (H_q / H_kv);
-  const long long tiles = rows / kRows + B;
-  if (rows > INT_MAX / 2 || B > INT_MAX / 2 || tiles * H_kv > (1 << 23) || split_tiles(T, B) * H_kv > (1 << 23))
+  long long tiles = rows / kRows + B;  // of whole blocks
+  if (rows > INT_MAX / 2 || B > INT_MAX / 2 || 2 * tiles * H_kv > (1 << 23) || split_tiles(T, B) * H_kv > (1 << 23))
     return SAKI_ERR_UNSUPPORTED;
   if (T == 0 || B == 0) return SAKI_OK;
   if (!cu || !out || reinterpret_cast<uintptr_t>(out) % 16 || !rows_ok(q, ld_q, H_q, dtype) ||
       !rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(v, ld_v, H_kv, dtype))
     return SAKI_ERR_ARG;
   if (ld_q > kMaxLd || ld_k > kMaxLd || ld_v > kMaxLd) return SAKI_ERR_UNSUPPORTED;
+  const bool halves = halves_better(tiles * H_kv, T, B);
+  if (halves) tiles = rows / (kRows / 2) + B;
   const PromptArgs a{q, k, v, ld_q, ld_k, ld_v, cu, B, H_q, H_kv, T, out, (int)tiles};
   const dim3 grid((unsigned)(tiles * H_kv));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (dtype == SAKI_BF16) {
-    hipLaunchKernelGGL(prompt_attend_kernel, grid, dim3(256), 0, s, a);
+    if (halves)
+      hipLaunchKernelGGL((prompt_attend_kernel<2>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((prompt_attend_kernel<1>), grid, dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? SAKI_OK : SAKI_ERR_HIP;
   }
   if (!ws || ws_bytes < saki_attend_prompt_workspace_bytes(dtype, T, B, H_kv) || reinterpret_cast<uintptr_t>(ws) % 16)
@@ -513,7 +602,12 @@ int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, i
   int2* exps = (int2*)(parts + (size_t)n * kSplitTile);
   hipLaunchKernelGGL(prompt_split_kernel, dim3((unsigned)n), dim3(256), 0, s, a, parts, exps);
   if (hipGetLastError() != hipSuccess) return SAKI_ERR_HIP;
-  hipLaunchKernelGGL(prompt_attend_f32_kernel, grid, dim3(256), 0, s, a, (const uint8_t*)parts, (const int2*)exps);
+  if (halves)
+    hipLaunchKernelGGL((prompt_attend_f32_kernel<2>), grid, dim3(256), 0, s, a, (const uint8_t*)parts,
+                       (const int2*)exps);
+  else
+    hipLaunchKernelGGL((prompt_attend_f32_kernel<1>), grid, dim3(256), 0, s, a, (const uint8_t*)parts,
+                       (const int2*)exps);
   return hipGetLastError() == hipSuccess ? SAKI_OK : SAKI_ERR_HIP;
 }
 

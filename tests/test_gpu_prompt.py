@@ -48,6 +48,8 @@ def check(out, q, k, v, cu, dt):
 @pytest.mark.parametrize("lens,H_q,H_kv", [
     ([1], 1, 1), ([2], 32, 8), ([31, 33, 1], 4, 1), ([64], 8, 8), ([65, 0, 127, 128, 129], 4, 2),
     ([0, 0, 5], 28, 4), ([300], 12, 1), ([17, 400], 5, 5), ([1] * 40, 16, 2), ([255, 1, 256], 7, 1),
+    # more blocks than halves are taken for: every work-group of 128 rows
+    ([70, 1, 33, 130] * 3, 32, 8), ([5, 200] * 3, 40, 20),
 ])
 def test_attend_prompt(lens, H_q, H_kv, dt):
     cu = np.concatenate([[0], np.cumsum(lens)])
@@ -123,11 +125,12 @@ def test_attend_prompt_offsets_that_do_not_ascend_stay_in_range(dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_attend_prompt_long_rows_sampled(dt):
+@pytest.mark.parametrize("H_q,H_kv", [(8, 2), (16, 4)])  # halved blocks, whole ones
+def test_attend_prompt_long_rows_sampled(H_q, H_kv, dt):
     """A long prompt among short ones: sampled rows, against float64 on the GPU."""
     lens = [40, 5000, 1, 700]
     cu = np.concatenate([[0], np.cumsum(lens)])
-    q, k, v = make(cu[-1], 8, 2, dt, 5)
+    q, k, v = make(cu[-1], H_q, H_kv, dt, 5)
     tq, tk, tv = (dev(x, DT[dt]) for x in (q, k, v))
     got = host(S.saki_attend_prompt(tq, tk, tv, ints(cu)))
     rng = np.random.default_rng(6)
