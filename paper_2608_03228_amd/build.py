@@ -2,6 +2,7 @@
 
 The host calibration (C++17, float64) is compiled with g++ and the HIP
 kernels with hipcc; hipcc links both into paper_2608_03228_amd/libsaki.so.
+The Python binding's argument module (_saki_args) links to it.
 Run ``python -m paper_2608_03228_amd.build`` (or call ``build()``).
 """
 from __future__ import annotations
@@ -10,12 +11,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsaki.so")
+ARGS = os.path.join(PKG, "_saki_args" + sysconfig.get_config_var("EXT_SUFFIX"))
 BUILD_DIR = os.path.join(PKG, "_build")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -51,13 +54,26 @@ def build(verbose: bool = True) -> str:
     _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-pthread", host_o, *dev_o,
           "-o", tmp], verbose)
     os.replace(tmp, LIB)
+    build_args(verbose)
     return LIB
+
+
+def build_args(verbose: bool = True) -> str:
+    """Compile the binding's argument module against libsaki.so."""
+    tmp = ARGS + ".tmp"
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-Wextra",
+          "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
+          os.path.join(CSRC, "saki_args.cpp"), "-L", PKG, "-l:libsaki.so", "-Wl,-rpath,$ORIGIN",
+          "-o", tmp], verbose)
+    os.replace(tmp, ARGS)
+    return ARGS
 
 
 def clean():
     shutil.rmtree(BUILD_DIR, ignore_errors=True)
-    if os.path.exists(LIB):
-        os.remove(LIB)
+    for path in (LIB, ARGS):
+        if os.path.exists(path):
+            os.remove(path)
 
 
 if __name__ == "__main__":

@@ -562,49 +562,57 @@ __device__ __forceinline__ Share share_of(long long total, int groups) {
 // The codes are exact in bf16; queries (float32: three terms) and weights (two
 // terms, three for float32 output) are split so that nothing but the output is
 // rounded to bf16.  HBM bound: 16 KB a tile.
-template <bool F32>
+//
+// Without SPLIT a work-group takes one whole pair: no share to find, no
+// workspace and no join (see whole_better).
+template <bool F32, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const void* __restrict__ q, void* out,
                                                               float* __restrict__ ws) {
   constexpr int kQT = F32 ? 3 : 1, kPT = F32 ? 3 : 2;
-  __shared__ long long part[4], found[2];
   __shared__ float s_m[4][16], s_l[4][16], s_o[4][16][kHeadDim + 4];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int n = lane % 16, g = lane / 16;
   const int G = a.H_q / a.H_kv, R = G * a.Q, RB = (R + 15) / 16, pairs = a.H_kv * RB;
 
-  long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 256) {
-    const int t = b0 + tid < a.B ? tiles_of(a.lens[b0 + tid], a.max_blocks) : 0;
-    long long sum;
-    group_scan((long long)t * pairs, part, &sum);
-    total += sum;
+  long long cur = 0, end = 1, base = 0;  // the tiles to take, the tiles before request b
+  int b = blockIdx.x / pairs;
+  if constexpr (SPLIT) {
+    __shared__ long long part[4], found[2];
+    long long total = 0, mine = 0, upto = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 256) {
+      mine = b0 + tid < a.B ? (long long)tiles_of(a.lens[b0 + tid], a.max_blocks) * pairs : 0;
+      long long sum;
+      upto = group_scan(mine, part, &sum);
+      total += sum;
+    }
+    const Share sh = share_of(total, gridDim.x);
+    cur = sh.piece * blockIdx.x;
+    end = min(total, cur + sh.piece);
+    if (cur >= end) return;
+    for (int b0 = 0; b0 < a.B; b0 += 256) {
+      long long sum = total;
+      if (a.B > 256) {  // (else the sums above are the ones)
+        mine = b0 + tid < a.B ? (long long)tiles_of(a.lens[b0 + tid], a.max_blocks) * pairs : 0;
+        upto = base + group_scan(mine, part, &sum);
+      }
+      if (cur < upto && cur >= upto - mine) found[0] = b0 + tid, found[1] = upto - mine;
+      base += sum;
+      if (cur < base) break;
+    }
+    __syncthreads();
+    b = (int)found[0];
+    base = found[1];
   }
-  const Share sh = share_of(total, gridDim.x);
-  long long cur = sh.piece * blockIdx.x;
-  const long long end = min(total, cur + sh.piece);
-  if (cur >= end) return;
-  long long base = 0;  // tiles before request b
-  for (int b0 = 0; b0 < a.B; b0 += 256) {
-    const long long t = b0 + tid < a.B ? (long long)tiles_of(a.lens[b0 + tid], a.max_blocks) * pairs : 0;
-    long long sum;
-    const long long upto = base + group_scan(t, part, &sum);
-    if (cur < upto && cur >= upto - t) found[0] = b0 + tid, found[1] = upto - t;
-    base += sum;
-    if (cur < base) break;
-  }
-  __syncthreads();
-  int b = (int)found[0];
-  base = found[1];
 
   while (cur < end) {
     const int len = a.lens[b], nt = tiles_of(len, a.max_blocks);
-    if (cur >= base + (long long)nt * pairs) {
+    if (SPLIT && cur >= base + (long long)nt * pairs) {
       base += (long long)nt * pairs;
       if (++b >= a.B) return;  // (a later request has the tiles that are left)
       continue;
     }
-    const int pair = (int)((cur - base) / nt), t0 = (int)((cur - base) % nt);
-    const int t1 = (int)min((long long)nt, t0 + (end - cur));
+    const int pair = SPLIT ? (int)((cur - base) / nt) : blockIdx.x % pairs, t0 = SPLIT ? (int)((cur - base) % nt) : 0;
+    const int t1 = SPLIT ? (int)min((long long)nt, t0 + (end - cur)) : nt;
     const int hk = pair / RB, r0 = pair % RB * 16;
     const size_t row0 = ((size_t)b * a.H_q + (size_t)hk * G) * a.Q + r0;
 
@@ -726,7 +734,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
       }
     }
 
-    // the four waves' parts: lane (n, g) holds dims 8 (4 g + i) + j of row n in o[j][i]
+    // the waves' parts: lane (n, g) holds dims 8 (4 g + i) + j of row n in o[j][i]
     l += xor_f32(l, 16);
     l += xor_f32(l, 32);
     __syncthreads();  // the last stretch's parts are read
@@ -738,8 +746,11 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
       *reinterpret_cast<float4*>(p + 4) = make_float4(o[4][i], o[5][i], o[6][i], o[7][i]);
     }
     __syncthreads();
-    const int row = tid / 16, d0 = tid % 16 * 8;
-    float M = -INFINITY, L = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int kDims = 8;  // of a thread
+    const int row = tid / 16, d0 = tid % 16 * kDims;
+    float M = -INFINITY, L = 0.f, y[kDims];
+#pragma unroll
+    for (int j = 0; j < kDims; ++j) y[j] = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) M = fmaxf(M, s_m[w][row]);
 #pragma unroll
@@ -747,31 +758,33 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
       const float e = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][row] - M);
       L += s_l[w][row] * e;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] += s_o[w][row][d0 + j] * e;
+      for (int j = 0; j < kDims; ++j) y[j] += s_o[w][row][d0 + j] * e;
     }
     if (r0 + row < R) {
-      if (t0 == 0 && t1 == nt) {
+      if (!SPLIT || (t0 == 0 && t1 == nt)) {
         const float inv = L > 0.f ? 1.f / L : 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= inv;
         const size_t to = (row0 + row) * kHeadDim + d0;
+#pragma unroll
+        for (int j = 0; j < kDims; ++j) y[j] *= inv;
         if constexpr (F32)
-          store_elems<float, 8>((float*)out + to, y);
+          store_elems<float, kDims>((float*)out + to, y);
         else
-          store_elems<__bf16, 8>((__bf16*)out + to, y);
-      } else {  // a share has two such stretches at most: one that began before it, one that ends after it
+          store_elems<__bf16, kDims>((__bf16*)out + to, y);
+      } else if constexpr (SPLIT) {  // a share has two such stretches at most: one that began before it, one that ends after it
         float* p = ws + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartFloats;
-        store_elems<float, 8>(p + row * kHeadDim + d0, y);
+        store_elems<float, kDims>(p + row * kHeadDim + d0, y);
         if (d0 == 0) p[kPartRows * kHeadDim + row] = M, p[kPartRows * kHeadDim + kPartRows + row] = L;
       }
     }
+    if (!SPLIT) break;
     cur += t1 - t0;
   }
 }
 
 // Joins the parts of the pairs that several work-groups shared, and writes
-// zeros for requests without a key.  One work-group per pair and 16 dims; its
-// four waves take every fourth part.
+// zeros for requests without a key.  A work-group takes 16 dims of a pair (all
+// dims, 16 at a time, where there are many pairs); its four waves take every
+// fourth part.
 template <bool F32>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups, const float* __restrict__ ws,
                                                          void* out) {
@@ -794,43 +807,47 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups
   const long long from = s_base + (long long)nt * pair;
   const int w0 = (int)(from / sh.piece), w1 = nt ? (int)((from + nt - 1) / sh.piece) : w0;
   if (nt && w0 == w1) return;
-  const int row = lane / 4, d0 = blockIdx.y * 16 + lane % 4 * 4;
+  const int row = lane / 4;
   const int hk = pair / RB, r0 = pair % RB * 16;
-  float M = -INFINITY, L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
   const bool in = r0 + row < R;
-  if (nt && in)
-    for (int w = w0 + wave; w <= w1; w += 4) {
-      const float* p = ws + ((size_t)w * 2 + (w == w0)) * kPartFloats;
-      const float m = p[kPartRows * kHeadDim + row], l = p[kPartRows * kHeadDim + kPartRows + row];
-      const float4 x = *reinterpret_cast<const float4*>(p + row * kHeadDim + d0);
-      const float m1 = fmaxf(M, m), ref = m1 == -INFINITY ? 0.f : m1;
-      const float e0 = __builtin_amdgcn_exp2f(M - ref), e1 = __builtin_amdgcn_exp2f(m - ref);
-      M = m1;
-      L = L * e0 + l * e1;
-      y[0] = y[0] * e0 + x.x * e1, y[1] = y[1] * e0 + x.y * e1;
-      y[2] = y[2] * e0 + x.z * e1, y[3] = y[3] * e0 + x.w * e1;
+  for (int part16 = blockIdx.y; part16 < kHeadDim / 16; part16 += gridDim.y) {
+    const int d0 = part16 * 16 + lane % 4 * 4;
+    float M = -INFINITY, L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    if (nt && in)
+      for (int w = w0 + wave; w <= w1; w += 4) {
+        const float* p = ws + ((size_t)w * 2 + (w == w0)) * kPartFloats;
+        const float m = p[kPartRows * kHeadDim + row], l = p[kPartRows * kHeadDim + kPartRows + row];
+        const float4 x = *reinterpret_cast<const float4*>(p + row * kHeadDim + d0);
+        const float m1 = fmaxf(M, m), ref = m1 == -INFINITY ? 0.f : m1;
+        const float e0 = __builtin_amdgcn_exp2f(M - ref), e1 = __builtin_amdgcn_exp2f(m - ref);
+        M = m1;
+        L = L * e0 + l * e1;
+        y[0] = y[0] * e0 + x.x * e1, y[1] = y[1] * e0 + x.y * e1;
+        y[2] = y[2] * e0 + x.z * e1, y[3] = y[3] * e0 + x.w * e1;
+      }
+    __syncthreads();  // the last dims are read
+    s_m[wave][row] = M, s_l[wave][row] = L;  // equal from a row's four lanes
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s_y[wave][row][lane % 4 * 4 + j] = y[j];
+    __syncthreads();
+    const int r = tid / 16, d = tid % 16;
+    if (r0 + r >= R) continue;
+    M = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+    float sum = 0.f;
+    L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float e = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - M);
+      L += s_l[w][r] * e;
+      sum += s_y[w][r][d] * e;
     }
-  s_m[wave][row] = M, s_l[wave][row] = L;  // equal from a row's four lanes
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s_y[wave][row][lane % 4 * 4 + j] = y[j];
-  __syncthreads();
-  const int r = tid / 16, d = tid % 16;
-  if (r0 + r >= R) return;
-  M = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
-  float sum = 0.f;
-  L = 0.f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float e = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - M);
-    L += s_l[w][r] * e;
-    sum += s_y[w][r][d] * e;
+    sum = L > 0.f ? sum / L : 0.f;
+    const size_t to = (((size_t)b * a.H_q + (size_t)hk * G) * a.Q + r0 + r) * kHeadDim + part16 * 16 + d;
+    if constexpr (F32)
+      ((float*)out)[to] = sum;
+    else
+      ((__bf16*)out)[to] = (__bf16)sum;
   }
-  sum = L > 0.f ? sum / L : 0.f;
-  const size_t to = (((size_t)b * a.H_q + (size_t)hk * G) * a.Q + r0 + r) * kHeadDim + blockIdx.y * 16 + d;
-  if constexpr (F32)
-    ((float*)out)[to] = sum;
-  else
-    ((__bf16*)out)[to] = (__bf16)sum;
 }
 
 // Attention over listed keys: one wave per (request, head, query) row.  Lane e
@@ -1037,12 +1054,32 @@ int saki_cache_write(const void* k, const void* v, int dtype, int T, int H_kv, i
   return launched() ? SAKI_OK : SAKI_ERR_HIP;
 }
 
+}  // extern "C"
+
+namespace {
+
+// Whether a work-group takes a whole pair: the lengths are read on the device,
+// so the tables' width has to bound a group's time.  us (bf16, 32 / 8 heads),
+// split and joined / whole pairs, for requests of the full width:
+//               4 tiles      8          16          32          64
+//    1 request   9.3 / 5.7  10.5 / 7.6  10.7 / 10.8  11.0 / 17.2  11.9 / 29.6
+//    8           9.7 / 5.8  10.9 / 7.7  11.2 / 10.9  14.7 / 18.8
+//   64          16.9 / 8.5  22.4 / 14.5 32.4 / 24.0  52.2 / 43.3
+//  256          49.8 / 26.1             119 / 101
+// (512 pairs and more fill the GPU without being split, up to the width where
+// one long request among short ones would keep a group alone at work).
+bool whole_better(long long pairs, int max_blocks) { return max_blocks <= (pairs >= 512 ? 32 : 16); }
+
+}  // namespace
+
+extern "C" {
+
 size_t saki_cache_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int max_blocks, int k) {
   if (B <= 0 || H_q <= 0 || H_kv <= 0 || H_q % H_kv != 0 || Q < 0 || Q > SAKI_CACHE_MAX_Q || max_blocks <= 0 || k < 0 ||
       k > saki::kMaxK)
     return 0;
-  if (k > 0 || Q == 0) return 256;
   const long long row_blocks = ((long long)(H_q / H_kv) * Q + 15) / 16;
+  if (k > 0 || Q == 0 || whole_better(B * H_kv * row_blocks, max_blocks)) return 256;
   const double tiles = (double)B * H_kv * row_blocks * max_blocks;
   const int groups = attend_groups(tiles > 1e9 ? 1000000000LL : (long long)tiles);
   return (size_t)groups * 2 * kPartFloats * sizeof(float);
@@ -1075,16 +1112,25 @@ int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q,
       hipLaunchKernelGGL((cache_lists_kernel<false>), grid, dim3(256), 0, s, a, q, top_idx, k, rows, out);
     return launched() ? SAKI_OK : SAKI_ERR_HIP;
   }
+  const long long pairs = B * H_kv * row_blocks;
+  if (whole_better(pairs, max_blocks)) {
+    const dim3 grid((unsigned)pairs);
+    if (dtype == SAKI_F32)
+      hipLaunchKernelGGL((cache_attend_kernel<true, false>), grid, dim3(256), 0, s, a, q, out, nullptr);
+    else
+      hipLaunchKernelGGL((cache_attend_kernel<false, false>), grid, dim3(256), 0, s, a, q, out, nullptr);
+    return launched() ? SAKI_OK : SAKI_ERR_HIP;
+  }
   const size_t need = saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, 0);
   if (!ws || ws_bytes < need || !aligned(ws, 16)) return SAKI_ERR_WORKSPACE;
   const int groups = (int)(need / (2 * kPartFloats * sizeof(float)));
-  const dim3 join((unsigned)((long long)B * H_kv * row_blocks), kHeadDim / 16);
+  const dim3 join((unsigned)pairs, pairs >= 256 ? 1 : kHeadDim / 16);
   if (dtype == SAKI_F32) {
-    hipLaunchKernelGGL((cache_attend_kernel<true>), dim3(groups), dim3(256), 0, s, a, q, out, (float*)ws);
+    hipLaunchKernelGGL((cache_attend_kernel<true, true>), dim3(groups), dim3(256), 0, s, a, q, out, (float*)ws);
     if (!launched()) return SAKI_ERR_HIP;
     hipLaunchKernelGGL((cache_join_kernel<true>), join, dim3(256), 0, s, a, groups, (const float*)ws, out);
   } else {
-    hipLaunchKernelGGL((cache_attend_kernel<false>), dim3(groups), dim3(256), 0, s, a, q, out, (float*)ws);
+    hipLaunchKernelGGL((cache_attend_kernel<false, true>), dim3(groups), dim3(256), 0, s, a, q, out, (float*)ws);
     if (!launched()) return SAKI_ERR_HIP;
     hipLaunchKernelGGL((cache_join_kernel<false>), join, dim3(256), 0, s, a, groups, (const float*)ws, out);
   }

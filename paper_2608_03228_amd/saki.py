@@ -418,11 +418,30 @@ def saki_attend(values, q, top_idx, N_valid: int, keys=None, index=None, sketch:
 
 CACHE_BLOCK = 64    # tokens per cache block
 CACHE_MAX_Q = 16    # queries per request and head in saki_cache_attend
+NO_WORKSPACE = 256  # a workspace size up to this: the call needs none
 
-# These calls run 4 to 10 us on the GPU for a decode step, as long as a dozen
-# checked arguments take in Python; so each argument is checked once, by as few
-# attribute reads as tell that it is right, and looked at again only to say
-# what is wrong with it (10.4 us a call before, see the checks below).
+# These calls run 4 to 10 us on the GPU for a decode step, less than a dozen
+# checked arguments take in Python: the checks and conversions that pass are made
+# by a module in C++ (csrc/saki_args.cpp), and an argument that does not is
+# looked at again here to say what is wrong with it.
+_args_mod = None
+_codes = {}
+
+
+def _args():
+    """The module; loading it fails if it has not been built."""
+    global _args_mod
+    if _args_mod is None:
+        lib()
+        try:
+            from . import _saki_args
+        except ImportError as e:
+            raise RuntimeError("paper_2608_03228_amd/_saki_args is missing or does not load "
+                               f"({e}); build it with `python -m paper_2608_03228_amd.build`") from e
+        torch = _torch()
+        _codes.update({torch.float32: F32, torch.bfloat16: BF16})
+        _args_mod = _saki_args
+    return _args_mod
 
 
 def _current():
@@ -436,11 +455,24 @@ def _current():
 
 def _array(t, dtype, shape, dev, name):
     """A dense tensor of this type and shape on the current device -> pointer."""
-    try:
-        if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
-            return t.data_ptr()
-    except AttributeError:
-        pass
+    p = _args_mod.array(t, dtype, shape, dev)
+    if p is None:
+        _refuse(t, dtype, shape, dev, name)
+        raise ValueError(f"{name} must be contiguous")
+    return p
+
+
+def _rows(t, dtype, shape, dev, name):
+    """Token rows [T, H, d] whose heads are dense -> pointer, elements between tokens."""
+    r = _args_mod.rows(t, dtype, shape, dev)
+    if r is None:
+        _refuse(t, dtype, shape, dev, name)
+        raise ValueError(f"{name} must have dense heads in rows that do not overlap, got strides "
+                         f"{tuple(t.stride())}")
+    return r
+
+
+def _refuse(t, dtype, shape, dev, name):
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype != dtype:
@@ -449,37 +481,21 @@ def _array(t, dtype, shape, dev, name):
         raise ValueError(f"{name} is on {t.device}, not on the current device (cuda:{dev})")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    raise ValueError(f"{name} must be contiguous")
-
-
-def _rows(t, dtype, shape, dev, name):
-    """Token rows [T, H, d] whose heads are dense -> pointer, elements between tokens."""
-    T, H, d = shape
-    try:
-        if t.dtype is dtype and t.get_device() == dev and t.shape == shape:
-            if t.is_contiguous():
-                return t.data_ptr(), H * d
-            sT, sH, sd = t.stride()
-            if (sd == 1 or d == 1) and (sH == d or H == 1) and (sT >= H * d or T == 1):
-                return t.data_ptr(), sT if T > 1 else H * d
-            raise ValueError(f"{name} must have dense heads in rows that do not overlap, got "
-                             f"strides {(sT, sH, sd)}")
-    except AttributeError:
-        pass
-    return _array(t, dtype, shape, dev, name), H * d
 
 
 def _of_floats(t, dims, name):
     """-> shape, torch dtype and library dtype of a float32 or bf16 tensor."""
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    _args()
+    if not isinstance(t, _torch_mod.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     dt = t.dtype
-    if dt is not torch.bfloat16 and dt is not torch.float32:
+    code = _codes.get(dt)
+    if code is None:
         raise ValueError(f"{name} has dtype {dt}, expected float32 or bfloat16")
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
-    return t.shape, dt, BF16 if dt is torch.bfloat16 else F32
+    shape = t.shape
+    if len(shape) != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {len(shape)}")
+    return shape, dt, code
 
 
 def _cache_arrays(k_cache, v_cache, scales, dev):
@@ -508,7 +524,7 @@ _section_arrays = {}
 
 
 def _sections(sections, axes, d):
-    """The host array of the sections (one per distinct tuple, at most 256)."""
+    """The sections as a host array (one per distinct tuple, at most 256)."""
     if sections is None and axes == 1:
         sections = (d // 2,)
     if sections is None or len(sections) != axes:
@@ -517,6 +533,7 @@ def _sections(sections, axes, d):
     a = _section_arrays.get(key)
     if a is None:
         a = (C.c_int * axes)(*key)
+        a.address = C.addressof(a)
         if len(_section_arrays) < 256:
             _section_arrays[key] = a
     return a
@@ -551,7 +568,7 @@ def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse:
         ko, ldko = (kp, ldk) if k_out is k else _rows(k_out, dt, kshape, dev, "k_out")
     else:
         k_out = None
-    st = lib().saki_rope(qp, kp, code, T, H_q, H_kv, d, ldq, ldk, pp, axes, sec, rope_theta,
+    st = _args_mod.saki_rope(qp, kp, code, T, H_q, H_kv, d, ldq, ldk, pp, axes, sec.address, rope_theta,
                          1 if inverse else 0, qo, ko, ldqo, ldko,
                          cur if stream is None else stream.cuda_stream)
     if st:
@@ -564,11 +581,12 @@ def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=No
     """ctx_lens, new_lens [B], free_blocks [n_free], tables [B, max_blocks] (in
     place), slots and pos [T] (outputs), all int32 CUDA.  Returns (tables,
     slots, pos, cu [B + 1], lens [B], counts [2])."""
+    _args()
     if not tables.is_cuda:
         raise ValueError("tables must be a CUDA (HIP) tensor")
     torch, dev, cur = _current()
     i32 = torch.int32
-    if tables.dim() != 2 or slots.dim() != 1 or free_blocks.dim() != 1:
+    if len(tables.shape) != 2 or len(slots.shape) != 1 or len(free_blocks.shape) != 1:
         raise ValueError("tables must be [B, max_blocks], slots [T] and free_blocks [n_free]")
     B, max_blocks = tables.shape
     T, n_free = slots.shape[0], free_blocks.shape[0]
@@ -578,7 +596,7 @@ def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=No
         lens = _new(stream, (B,), i32, tables.device)
     if counts is None:
         counts = _new(stream, (2,), i32, tables.device)
-    st = lib().saki_block_tables(
+    st = _args_mod.saki_block_tables(
         _array(ctx_lens, i32, (B,), dev, "ctx_lens"), _array(new_lens, i32, (B,), dev, "new_lens"),
         B, _array(free_blocks, i32, (n_free,), dev, "free_blocks"), n_free,
         _array(tables, i32, (B, max_blocks), dev, "tables"), max_blocks,
@@ -601,7 +619,7 @@ def saki_cache_write(k, v, slots, k_cache, v_cache, scales, stream=None):
     shape = (T, H_kv, d)
     kp, ldk = _rows(k, dt, shape, dev, "k")
     vp_, ldv = _rows(v, dt, shape, dev, "v")
-    st = lib().saki_cache_write(kp, vp_, code, T, H_kv, d, ldk, ldv,
+    st = _args_mod.saki_cache_write(kp, vp_, code, T, H_kv, d, ldk, ldv,
                                 _array(slots, torch.int32, (T,), dev, "slots"), kc, vc, sc, n_blocks,
                                 cur if stream is None else stream.cuda_stream)
     if st:
@@ -640,11 +658,13 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
         ip = _array(top_idx, torch.int32, (B, H_q, Q, k), dev, "top_idx")
     else:
         if ws is None:
-            need = saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks)
-            ws = _new(stream, max(need, 1), torch.uint8, q.device)
-        wn = ws.numel()
-        wp = _array(ws, torch.uint8, (wn,), dev, "ws")
-    st = lib().saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
+            need = _args_mod.saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, 0)
+            if need > NO_WORKSPACE:
+                ws = _new(stream, need, torch.uint8, q.device)
+        if ws is not None:
+            wn = ws.numel()
+            wp = _array(ws, torch.uint8, (wn,), dev, "ws")
+    st = _args_mod.saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
                                  lp, ip, k, op, wp, wn, cur if stream is None else stream.cuda_stream)
     if st:
         _check("saki_cache_attend", st)
@@ -675,12 +695,12 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
         out = _new(stream, shape, dt, q.device)
     wp, wn = None, 0
     if ws is None and code == F32:
-        need = lib().saki_attend_prompt_workspace_bytes(F32, T, n - 1, H_kv)
+        need = _args_mod.saki_attend_prompt_workspace_bytes(F32, T, n - 1, H_kv)
         ws = _new(stream, max(need, 1), torch.uint8, q.device)
     if ws is not None:
         wn = ws.numel()
         wp = _array(ws, torch.uint8, (wn,), dev, "ws")
-    st = lib().saki_attend_prompt(qp, kp, vp_, code, T, n - 1, H_q, H_kv, d, ldq, ldk, ldv, cp,
+    st = _args_mod.saki_attend_prompt(qp, kp, vp_, code, T, n - 1, H_q, H_kv, d, ldq, ldk, ldv, cp,
                                   _array(out, dt, shape, dev, "out"), wp, wn,
                                   cur if stream is None else stream.cuda_stream)
     if st:

@@ -284,19 +284,21 @@ def check_attend(case, lens, dt, top_idx=None, **kw):
 @pytest.mark.parametrize("lens,H_q,H_kv,Q", [
     ([1], 1, 1, 1), ([63], 4, 1, 1), ([64], 8, 2, 1), ([65], 28, 4, 1), ([0, 5, 0], 4, 2, 1),
     ([0], 2, 1, 3), ([1000], 32, 8, 1), ([300, 1, 640, 129], 12, 1, 4), ([3, 200], 5, 5, 16),
-    ([2], 4, 2, 16), ([700, 699], 17, 1, 1), ([-4, 70], 2, 1, 2),
+    ([2], 4, 2, 16), ([700, 699], 17, 1, 1), ([-4, 70], 2, 1, 2), ([1500, 300], 4, 1, 1),
 ])
-def test_cache_attend(lens, H_q, H_kv, Q, dt):
-    check_attend(attend_case(lens, H_q, H_kv, Q, dt), lens, dt)
+@pytest.mark.parametrize("rows", [None, 40])  # narrow tables: a work-group per pair; wide ones: shares, joined
+def test_cache_attend(rows, lens, H_q, H_kv, Q, dt):
+    check_attend(attend_case(lens, H_q, H_kv, Q, dt, rows), lens, dt)
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_cache_attend_many_requests(dt):
+@pytest.mark.parametrize("rows", [15, 40])
+def test_cache_attend_many_requests(rows, dt):
     """More requests than one scan step takes, most of them short."""
     rng = np.random.default_rng(0)
     lens = rng.integers(0, 70, 530).tolist()
     lens[400] = 900
-    check_attend(attend_case(lens, 2, 2, 1, dt), lens, dt)
+    check_attend(attend_case(lens, 2, 2, 1, dt, rows), lens, dt)
 
 
 def test_cache_attend_table_entries_out_of_range():
@@ -337,6 +339,7 @@ def test_cache_attend_peaked_rows(top_idx):
 def test_cache_attend_is_the_same_every_time_and_on_another_stream():
     lens = [3000, 10, 700, 2500]
     q, codes, scales, (k, v, s), tab = attend_case(lens, 28, 4, 1, "bf16")
+    assert tab.shape[1] > 32  # shares and their join
     args = (dev(q, torch.bfloat16), k, v, s, ints(tab), ints(lens))
     first = S.saki_cache_attend(*args)
     side = torch.cuda.Stream()

@@ -83,7 +83,7 @@ ATTEND = ("q dtype B H_q H_kv Q d k_cache v_cache scales n_blocks tables max_blo
     (dict(B=1 << 23), UNSUP), (dict(B=1 << 24, top_idx=P, k=4), UNSUP),
 ])
 def test_cache_attend(lib, kw, status):
-    good = [P, 1, 2, 4, 2, 1, 128, P, P, P, 9, P, 8, P, None, 0, P, P, 1 << 30, None]
+    good = [P, 1, 2, 4, 2, 1, 128, P, P, P, 9, P, 80, P, None, 0, P, P, 1 << 30, None]
     assert change(lib.saki_cache_attend, good, ATTEND, **kw) == status
 
 
