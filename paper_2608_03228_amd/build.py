@@ -59,11 +59,17 @@ def build(verbose: bool = True) -> str:
 
 
 def build_args(verbose: bool = True) -> str:
-    """Compile the binding's argument module against libsaki.so."""
+    """Compile the binding's argument module against libsaki.so and torch."""
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
     tmp = ARGS + ".tmp"
+    inc = [f for p in include_paths() for f in ("-isystem", p)]
+    libs = [f for p in library_paths() for f in ("-L", p)]
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-Wextra",
-          "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
-          os.path.join(CSRC, "saki_args.cpp"), "-L", PKG, "-l:libsaki.so", "-Wl,-rpath,$ORIGIN",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, *inc,
+          "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "saki_args.cpp"),
+          "-L", PKG, "-l:libsaki.so", "-Wl,-rpath,$ORIGIN", *libs, "-ltorch_python", "-ltorch_cpu",
+          "-lc10",
           "-o", tmp], verbose)
     os.replace(tmp, ARGS)
     return ARGS

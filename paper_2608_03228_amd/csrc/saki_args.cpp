@@ -1,20 +1,26 @@
 // Argument marshalling of the Python binding's serving calls, as a CPython
 // module (_saki_args): what a decode step calls takes 4 to 10 us on the GPU, and
 // checking a call's tensors and converting its arguments took 6 us in Python
-// and ctypes (1.5 here).
+// and ctypes (1 here, where the tensors are read through torch's C++ types).
 //
-//   array(t, dtype, shape, dev)  data pointer of a dense tensor of this type and
-//                                shape on this device, None if it is not one
-//   rows(t, dtype, shape, dev)   (data pointer, elements between tokens) of token
-//                                rows [T, H, d] with dense heads, None likewise
+//   array(t, dtype, shape, dev, name)  data pointer of a dense tensor of this
+//                                type and shape on this device
+//   rows(t, dtype, shape, dev, name)   (data pointer, elements between tokens) of
+//                                token rows [T, H, d] with dense heads
+//   refusal(f)                   what array and rows call, with their arguments,
+//                                for a tensor that is not so; it raises
 //   saki_...(...)                the C entry points: None or an int for a pointer,
 //                                ints and floats for numbers; the status or size
 
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <torch/csrc/Dtype.h>
+#include <torch/csrc/autograd/python_variable.h>
+
 #include <climits>
 #include <cstdint>
+#include <exception>
 #include <tuple>
 #include <type_traits>
 #include <utility>
@@ -23,75 +29,81 @@
 
 namespace {
 
-PyObject *s_dtype, *s_shape, *s_get_device, *s_is_contiguous, *s_data_ptr, *s_stride;
+PyObject* g_refusal = nullptr;
 
-struct Ref {  // an owned reference
-  PyObject* p;
-  explicit Ref(PyObject* o) : p(o) {}
-  Ref(const Ref&) = delete;
-  Ref& operator=(const Ref&) = delete;
-  ~Ref() { Py_XDECREF(p); }
-};
-
-// Whether t has this dtype and shape and lies on this device; -1 on an error.
-int matches(PyObject* t, PyObject* dtype, PyObject* shape, PyObject* dev) {
-  Ref d(PyObject_GetAttr(t, s_dtype));
-  if (!d.p) return -1;
-  if (d.p != dtype) return 0;
-  Ref g(PyObject_CallMethodNoArgs(t, s_get_device));
-  if (!g.p) return -1;
-  int same = PyObject_RichCompareBool(g.p, dev, Py_EQ);
-  if (same != 1) return same;
-  Ref s(PyObject_GetAttr(t, s_shape));
-  if (!s.p) return -1;
-  return PyObject_RichCompareBool(s.p, shape, Py_EQ);
+PyObject* refuse(PyObject* const* a) {
+  if (g_refusal) {
+    PyObject* r = PyObject_Vectorcall(g_refusal, a, 5, nullptr);
+    Py_XDECREF(r);
+  }
+  if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an argument is not the tensor that is wanted");
+  return nullptr;
 }
 
-int contiguous(PyObject* t) {
-  Ref c(PyObject_CallMethodNoArgs(t, s_is_contiguous));
-  return c.p ? PyObject_IsTrue(c.p) : -1;
+// The tensor if it has this dtype and shape and lies on this device.
+const at::Tensor* matching(PyObject* const* a) {
+  if (!THPVariable_Check(a[0]) || !THPDtype_Check(a[1]) || !PyTuple_Check(a[2])) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(a[0]);
+  if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.is_neg() || t.is_conj() ||
+      t.scalar_type() != reinterpret_cast<THPDtype*>(a[1])->scalar_type)
+    return nullptr;
+  const long dev = PyLong_AsLong(a[3]);
+  const Py_ssize_t n = PyTuple_GET_SIZE(a[2]);
+  if (t.get_device() != dev || t.dim() != n) return nullptr;
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (t.size(i) != PyLong_AsLongLong(PyTuple_GET_ITEM(a[2], i))) return nullptr;
+  return &t;
 }
 
-// The caller looks again, and says what is wrong, where this is None.
-PyObject* none() {
-  PyErr_Clear();
+// torch's accessors throw for tensors without memory of their own.
+template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
+PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    return F(a, n);
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (...) {
+    PyErr_SetString(PyExc_ValueError, "an argument has no memory to point to");
+  }
+  return nullptr;
+}
+
+PyObject* array(PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "array takes 5 arguments");
+    return nullptr;
+  }
+  const at::Tensor* t = matching(a);
+  if (PyErr_Occurred()) return nullptr;
+  return t && t->is_contiguous() ? PyLong_FromVoidPtr(t->data_ptr()) : refuse(a);
+}
+
+PyObject* rows(PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "rows takes 5 arguments");
+    return nullptr;
+  }
+  const at::Tensor* t = matching(a);
+  if (PyErr_Occurred()) return nullptr;
+  if (!t || t->dim() != 3) return refuse(a);
+  const int64_t T = t->size(0), H = t->size(1), d = t->size(2);
+  int64_t ld = H * d;
+  if (!t->is_contiguous()) {
+    if ((t->stride(2) != 1 && d != 1) || (t->stride(1) != d && H != 1) || (t->stride(0) < ld && T != 1))
+      return refuse(a);
+    if (T > 1) ld = t->stride(0);
+  }
+  PyObject *p = PyLong_FromVoidPtr(t->data_ptr()), *l = PyLong_FromLongLong(ld);
+  PyObject* r = p && l ? PyTuple_Pack(2, p, l) : nullptr;
+  Py_XDECREF(p);
+  Py_XDECREF(l);
+  return r;
+}
+
+PyObject* refusal(PyObject*, PyObject* f) {
+  Py_INCREF(f);
+  Py_XSETREF(g_refusal, f);
   Py_RETURN_NONE;
-}
-
-PyObject* array(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "array takes 4 arguments");
-    return nullptr;
-  }
-  if (matches(a[0], a[1], a[2], a[3]) != 1 || contiguous(a[0]) != 1) return none();
-  return PyObject_CallMethodNoArgs(a[0], s_data_ptr);
-}
-
-PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4 || !PyTuple_Check(a[2]) || PyTuple_GET_SIZE(a[2]) != 3) {
-    PyErr_SetString(PyExc_TypeError, "rows takes 4 arguments, the third of 3 sizes");
-    return nullptr;
-  }
-  if (matches(a[0], a[1], a[2], a[3]) != 1) return none();
-  long long size[3], st[3];
-  for (int i = 0; i < 3; ++i) {
-    size[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(a[2], i));
-    if (size[i] < 0 || size[i] > INT_MAX) return none();
-  }
-  long long ld = size[1] * size[2];
-  const int dense = contiguous(a[0]);
-  if (dense < 0) return none();
-  if (!dense) {
-    Ref s(PyObject_CallMethodNoArgs(a[0], s_stride));
-    if (!s.p || !PyTuple_Check(s.p) || PyTuple_GET_SIZE(s.p) != 3) return none();
-    for (int i = 0; i < 3; ++i) st[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s.p, i));
-    if (PyErr_Occurred()) return none();
-    if ((st[2] != 1 && size[2] != 1) || (st[1] != size[2] && size[1] != 1) || (st[0] < ld && size[0] != 1))
-      return none();
-    if (size[0] > 1) ld = st[0];
-  }
-  Ref p(PyObject_CallMethodNoArgs(a[0], s_data_ptr));
-  return p.p ? Py_BuildValue("(OL)", p.p, ld) : nullptr;
 }
 
 template <typename T>
@@ -146,8 +158,9 @@ struct Entry<Fn> {
 
 #define SAKI_ENTRY(f) {#f, (PyCFunction)(void (*)(void))Entry<&f>::call, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    {"array", (PyCFunction)(void (*)(void))array, METH_FASTCALL, nullptr},
-    {"rows", (PyCFunction)(void (*)(void))rows, METH_FASTCALL, nullptr},
+    {"array", (PyCFunction)(void (*)(void))guarded<array>, METH_FASTCALL, nullptr},
+    {"rows", (PyCFunction)(void (*)(void))guarded<rows>, METH_FASTCALL, nullptr},
+    {"refusal", refusal, METH_O, nullptr},
     SAKI_ENTRY(saki_rope),
     SAKI_ENTRY(saki_block_tables),
     SAKI_ENTRY(saki_cache_write),
@@ -162,13 +175,4 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_saki_args", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__saki_args() {
-  s_dtype = PyUnicode_InternFromString("dtype");
-  s_shape = PyUnicode_InternFromString("shape");
-  s_get_device = PyUnicode_InternFromString("get_device");
-  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
-  s_data_ptr = PyUnicode_InternFromString("data_ptr");
-  s_stride = PyUnicode_InternFromString("stride");
-  if (!s_dtype || !s_shape || !s_get_device || !s_is_contiguous || !s_data_ptr || !s_stride) return nullptr;
-  return PyModule_Create(&module);
-}
+PyMODINIT_FUNC PyInit__saki_args() { return PyModule_Create(&module); }

@@ -425,14 +425,17 @@ NO_WORKSPACE = 256  # a workspace size up to this: the call needs none
 # by a module in C++ (csrc/saki_args.cpp), and an argument that does not is
 # looked at again here to say what is wrong with it.
 _args_mod = None
+_array = None  # (t, dtype, shape, dev, name) -> pointer of a dense tensor
+_rows = None   # the same -> pointer, elements between the tokens of [T, H, d] with dense heads
 _codes = {}
 
 
 def _args():
     """The module; loading it fails if it has not been built."""
-    global _args_mod
+    global _args_mod, _array, _rows
     if _args_mod is None:
         lib()
+        _torch()  # (the module's tensor types are torch's)
         try:
             from . import _saki_args
         except ImportError as e:
@@ -440,6 +443,8 @@ def _args():
                                f"({e}); build it with `python -m paper_2608_03228_amd.build`") from e
         torch = _torch()
         _codes.update({torch.float32: F32, torch.bfloat16: BF16})
+        _saki_args.refusal(_refuse)
+        _array, _rows = _saki_args.array, _saki_args.rows
         _args_mod = _saki_args
     return _args_mod
 
@@ -453,26 +458,8 @@ def _current():
     return torch, torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream
 
 
-def _array(t, dtype, shape, dev, name):
-    """A dense tensor of this type and shape on the current device -> pointer."""
-    p = _args_mod.array(t, dtype, shape, dev)
-    if p is None:
-        _refuse(t, dtype, shape, dev, name)
-        raise ValueError(f"{name} must be contiguous")
-    return p
-
-
-def _rows(t, dtype, shape, dev, name):
-    """Token rows [T, H, d] whose heads are dense -> pointer, elements between tokens."""
-    r = _args_mod.rows(t, dtype, shape, dev)
-    if r is None:
-        _refuse(t, dtype, shape, dev, name)
-        raise ValueError(f"{name} must have dense heads in rows that do not overlap, got strides "
-                         f"{tuple(t.stride())}")
-    return r
-
-
 def _refuse(t, dtype, shape, dev, name):
+    """Says what keeps a tensor from being the dense one that is wanted."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype != dtype:
@@ -481,6 +468,8 @@ def _refuse(t, dtype, shape, dev, name):
         raise ValueError(f"{name} is on {t.device}, not on the current device (cuda:{dev})")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name} must be contiguous (token rows: dense heads, rows that do not "
+                     f"overlap), got strides {tuple(t.stride())}")
 
 
 def _of_floats(t, dims, name):
