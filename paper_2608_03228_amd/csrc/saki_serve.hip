@@ -319,29 +319,31 @@ __device__ __forceinline__ int scale_exponent(float top) {
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
 // A run is a stretch of tokens whose slots ascend within one block; it belongs
-// to the window of tokens in which it begins.  One wave takes the runs of one
-// window for one head's keys or values and holds a whole run (up to 64 rows of
-// 512 bytes) in registers between the search for its largest element and the
-// rounding, all its loads in flight at once.  The block's scale is the least
-// power of two that covers the run, and, where the block holds tokens before
-// the run, no less than it was; if it grew, the codes before the run are moved
-// to it.  Powers of two make that exact but for codes that become subnormal,
-// and codes times scale exact in bf16.  HBM bound on prompts, latency on single
-// tokens.
+// to the window of tokens in which it begins.  One work-group takes the runs of
+// one window for one head's keys or values; each of its four waves holds 16 rows
+// of a run in registers between the search for the largest element and the
+// rounding, all its loads in flight at once (a wave with all 64 rows, 253
+// registers, reached 3.1 TB/s on prompts of float32 tokens).  The block's scale
+// is the least power of two that covers the run, and, where the block holds
+// tokens before the run, no less than it was; if it grew, the codes before the
+// run are moved to it.  Powers of two make that exact but for codes that become
+// subnormal, and codes times scale exact in bf16.  HBM bound on prompts, latency
+// on single tokens.
 template <typename T>
-__global__ __launch_bounds__(256, 2) void cache_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
-                                                             size_t ld_k, size_t ld_v, int n_tokens, int window,
-                                                             const int* __restrict__ slots, int n_blocks, int H,
-                                                             uint8_t* k_cache, uint8_t* v_cache, float* scales) {
-  constexpr int V = 16 / sizeof(T);         // elements a lane loads at once
-  constexpr int kLanes = kHeadDim / V;      // lanes a row
-  constexpr int kStep = kWave / kLanes;     // rows the wave loads at once
-  constexpr int kLoads = kTile / kStep, kGroup = 8;
-  const int lane = threadIdx.x % kWave, unit = blockIdx.y * 4 + threadIdx.x / kWave;
-  if (unit >= 2 * H) return;
-  const int h = unit >> 1, which = unit & 1;
+__global__ __launch_bounds__(256) void cache_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
+                                                          size_t ld_k, size_t ld_v, int n_tokens, int window,
+                                                          const int* __restrict__ slots, int n_blocks, int H,
+                                                          uint8_t* k_cache, uint8_t* v_cache, float* scales) {
+  constexpr int V = 16 / sizeof(T);      // elements a lane loads at once
+  constexpr int kLanes = kHeadDim / V;   // lanes a row
+  constexpr int kStep = kWave / kLanes;  // rows a wave loads at once
+  constexpr int kRows = kTile / 4, kLoads = kRows / kStep;
+  __shared__ float part[2][4];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int h = blockIdx.y >> 1, which = blockIdx.y & 1;
   const T* src = (which ? v : k) + (size_t)h * kHeadDim;
   const size_t ld = which ? ld_v : ld_k;
+  uint8_t* const cache = which ? v_cache : k_cache;
   const int n_slots = n_blocks * kTile;
   const int t0 = blockIdx.x * window;
   // tokens t0 - 1 .. t0 + 127: where runs begin and where they go on
@@ -357,10 +359,9 @@ __global__ __launch_bounds__(256, 2) void cache_write_kernel(const T* __restrict
   uint64_t begins = __ballot(lane < window && s0 >= 0 && s0 < n_slots && !on0);
   const uint64_t ones = begins & ~((on_a >> 1) | (on_b << (kWave - 1)));
   const int row = lane / kLanes, col = lane % kLanes * V;
-  uint8_t* const cache = which ? v_cache : k_cache;
   // moves the codes before slot `first` of a block to a grown scale
-  auto move = [&](uint8_t* block, int first, float ratio) {
-    for (int i = lane / 8; i < first; i += 8) {
+  auto move = [&](uint8_t* block, int first, float ratio, int from, int step) {
+    for (int i = from + lane / 8; i < first; i += step) {
       uint4* o = reinterpret_cast<uint4*>(block + i * kHeadDim + lane % 8 * 16);
       float y[16];
       decode16(*o, y);
@@ -368,21 +369,19 @@ __global__ __launch_bounds__(256, 2) void cache_write_kernel(const T* __restrict
     }
   };
 
-  // runs of one token (decode steps), a row of lanes each, up to 32 at once
-  constexpr int kBatch = kStep * kGroup;
-  for (int b = 0; b < window; b += kBatch) {
-    const uint64_t now_ones = ones >> b & ((1ull << kBatch) - 1);
-    if (!now_ones) continue;
-    uint4 x[kGroup];
-    int slot[kGroup];
-    float old[kGroup];
+  // runs of one token (decode steps): a row of lanes each, a quarter of the window a wave
+  const int b = wave * kRows;
+  if (const uint32_t mine = (uint32_t)(ones >> b) & ((1u << kRows) - 1)) {
+    uint4 x[kLoads];
+    int slot[kLoads];
+    float old[kLoads];
 #pragma unroll
-    for (int u = 0; u < kGroup; ++u) {
+    for (int u = 0; u < kLoads; ++u) {
       slot[u] = -1;
       x[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (now_ones >> (u * kStep) & ((1u << kStep) - 1)) {
+      if (mine >> (u * kStep) & ((1u << kStep) - 1)) {
         const int at = u * kStep + row, sl = __shfl(s0, b + at);
-        if (now_ones >> at & 1) {
+        if (mine >> at & 1) {
           slot[u] = sl;
           x[u] = *reinterpret_cast<const uint4*>(src + (size_t)(t0 + b + at) * ld + col);
           old[u] = scales[((size_t)(sl / kTile) * H + h) * 2 + which];
@@ -390,8 +389,8 @@ __global__ __launch_bounds__(256, 2) void cache_write_kernel(const T* __restrict
       }
     }
 #pragma unroll
-    for (int u = 0; u < kGroup; ++u)
-      if (now_ones >> (u * kStep) & ((1u << kStep) - 1)) {
+    for (int u = 0; u < kLoads; ++u)
+      if (mine >> (u * kStep) & ((1u << kStep) - 1)) {
         float y[V], top = 0.f, ratio = 0.f;
         unpack16<T>(x[u], y);
 #pragma unroll
@@ -416,66 +415,75 @@ __global__ __launch_bounds__(256, 2) void cache_write_kernel(const T* __restrict
           const int l = __builtin_ctzll(g);
           move(cache + ((size_t)__builtin_amdgcn_readlane(blk, l) * H + h) * kBlockBytes,
                __builtin_amdgcn_readlane(first, l),
-               __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(ratio), l)));
+               __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(ratio), l)), 0, 8);
         }
       }
   }
 
-  for (begins &= ~ones; begins; begins &= begins - 1) {
-    const int at = __builtin_ctzll(begins), t = t0 + at;
-    // the tokens after `at` that go on: at most 63, as a block's slots ascend
-    const uint64_t on = at == kWave - 1 ? on_b : (on_a >> (at + 1)) | (on_b << (kWave - 1 - at));
-    const int n = ~on ? 1 + __builtin_ctzll(~on) : kTile;
+  // The run of n tokens from t0 + at on, all waves together or one wave alone
+  int turn = 0;
+  auto take = [&](int at, int n, auto together) __attribute__((always_inline)) {
+    const int t = t0 + at, b = together ? wave * kRows : 0;
     const int slot = __builtin_amdgcn_readlane(s0, at);
     const int blk = slot / kTile, first = slot % kTile;
     uint8_t* out = cache + ((size_t)blk * H + h) * kBlockBytes;
     float* scale = scales + ((size_t)blk * H + h) * 2 + which;
     uint4 x[kLoads];
+    int to[kLoads];
     float top = 0.f;
-    const T* p = src + (size_t)(t + row) * ld + col;
 #pragma unroll
-    for (int g = 0; g < kLoads; g += kGroup)
-      if (g * kStep < n)
-#pragma unroll
-        for (int u = g; u < g + kGroup; ++u) {
-          x[u] = make_uint4(0u, 0u, 0u, 0u);
-          if (row + u * kStep < n) x[u] = *reinterpret_cast<const uint4*>(p + (size_t)(u * kStep) * ld);
-        }
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = b + u * kStep + row;
+      x[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (i < n) {
+        x[u] = *reinterpret_cast<const uint4*>(src + (size_t)(t + i) * ld + col);
+        to[u] = slots[t + i] % kTile;
+      }
+    }
     const float old = first ? *scale : 0.f;
 #pragma unroll
-    for (int g = 0; g < kLoads; g += kGroup)
-      if (g * kStep < n)
+    for (int u = 0; u < kLoads; ++u) {
+      float y[V];
+      unpack16<T>(x[u], y);
 #pragma unroll
-        for (int u = g; u < g + kGroup; ++u) {
-          float y[V];
-          unpack16<T>(x[u], y);
-#pragma unroll
-          for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(y[e]));
-        }
+      for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(y[e]));
+    }
 #pragma unroll
     for (int m = 1; m < kWave; m <<= 1) top = fmaxf(top, xor_f32(top, m));
+    if constexpr (together) {
+      if (lane == 0) part[turn][wave] = top;
+      __syncthreads();  // (the next run has the other half of `part`)
+      top = fmaxf(fmaxf(part[turn][0], part[turn][1]), fmaxf(part[turn][2], part[turn][3]));
+      turn ^= 1;
+    }
     const int e = scale_exponent(top);
     const bool grew = first && !(old >= pow2(e));
     const float now = first && !grew ? old : pow2(e);
     const float inv = first && !grew ? 1.f / now : pow2(-e);
 #pragma unroll
-    for (int g = 0; g < kLoads; g += kGroup)
-      if (g * kStep < n)
+    for (int u = 0; u < kLoads; ++u)
+      if (b + u * kStep + row < n) {
+        float y[V];
+        unpack16<T>(x[u], y);
+        uint32_t w[V / 4];
 #pragma unroll
-        for (int u = g; u < g + kGroup; ++u) {
-          const int i = row + u * kStep;
-          if (i < n) {
-            const int to = slots[t + i] % kTile;
-            float y[V];
-            unpack16<T>(x[u], y);
-            uint32_t w[V / 4];
-#pragma unroll
-            for (int j = 0; j < V / 4; ++j) w[j] = encode4(y + 4 * j, inv);
-            __builtin_memcpy(out + to * kHeadDim + col, w, V);
-          }
-        }
-    if (grew) move(out, first, old * inv);
-    if (lane == 0 && (!first || grew)) *scale = now;
+        for (int j = 0; j < V / 4; ++j) w[j] = encode4(y + 4 * j, inv);
+        __builtin_memcpy(out + to[u] * kHeadDim + col, w, V);
+      }
+    if (grew) move(out, first, old * inv, together ? 8 * wave : 0, together ? 32 : 8);
+    // (all waves that take part have read the scale, before the barrier above)
+    if (b == 0 && lane == 0 && (!first || grew)) *scale = now;
+  };
+  int alone = 0;
+  for (begins &= ~ones; begins; begins &= begins - 1) {
+    const int at = __builtin_ctzll(begins);
+    // the tokens after `at` that go on: at most 63, as a block's slots ascend
+    const uint64_t on = at == kWave - 1 ? on_b : (on_a >> (at + 1)) | (on_b << (kWave - 1 - at));
+    const int n = ~on ? 1 + __builtin_ctzll(~on) : kTile;
+    if (n > kRows)
+      take(at, n, std::true_type());
+    else if (alone++ % 4 == wave)  // (2,000 requests of 3 tokens: 43 us with all waves at each)
+      take(at, n, std::false_type());
   }
 }
 
@@ -958,7 +966,7 @@ bool launched() { return hipGetLastError() == hipSuccess; }
 // Blocks and heads of a cache: row numbers (64 tokens a block) fit an int.
 int check_cache(const void* k, const void* v, const void* scales, int n_blocks, int H_kv) {
   if (n_blocks < 0 || H_kv <= 0) return SAKI_ERR_ARG;
-  if ((long long)n_blocks * H_kv > INT_MAX / kTile || H_kv > 65535) return SAKI_ERR_UNSUPPORTED;
+  if ((long long)n_blocks * H_kv > INT_MAX / kTile || H_kv > 32767) return SAKI_ERR_UNSUPPORTED;
   if (n_blocks > 0 && (!k || !v || !scales || !aligned(k, 16) || !aligned(v, 16) || !aligned(scales, 8)))
     return SAKI_ERR_ARG;
   return SAKI_OK;
@@ -1040,10 +1048,10 @@ int saki_cache_write(const void* k, const void* v, int dtype, int T, int H_kv, i
   if (T == 0) return SAKI_OK;
   if (!slots || !rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(v, ld_v, H_kv, dtype)) return SAKI_ERR_ARG;
   if (n_blocks == 0) return SAKI_OK;  // no slot is within it
-  // about 4,096 waves, as many as the GPU holds twice; a window is one wave's
+  // some 2,000 work-groups (twice as many: 4,000 tokens of 8 heads 10.1 us in place of 7.1)
   int window = 1;
-  while (window < kWave && (long long)T * 2 * H_kv > 4096LL * window) window *= 2;
-  const dim3 grid((T + window - 1) / window, (2 * H_kv + 3) / 4);
+  while (window < kWave && (long long)T * 2 * H_kv > 2048LL * window) window *= 2;
+  const dim3 grid((T + window - 1) / window, 2 * H_kv);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (dtype == SAKI_F32)
     hipLaunchKernelGGL((cache_write_kernel<float>), grid, dim3(256), 0, s, (const float*)k, (const float*)v, ld_k,
