@@ -232,3 +232,42 @@ def test_attend_prompt_f32_of_very_different_sizes(what):
     bound = (2 * score + (T / 32 + 64) * U + 2.0 ** -21) * mass + 2.0 ** -37 * T * np.maximum(top, nxt) + U * np.abs(want)
     err = np.abs(host(out) - want)
     assert np.all(err <= bound), np.max(err / bound)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attend_prompt_rows_far_apart(dt):
+    """Token rows 2^22 elements apart: offsets of more than 4 GiB."""
+    T, H_q, H_kv = 600, 2, 1
+    q, k, v = make(T, H_q, H_kv, dt, 13)
+    cu = np.array([0, 20, T])
+    big = torch.empty(T * (1 << 22), dtype=DT[dt], device=DEV)
+    far = []
+    for i, x in enumerate((q, k, v)):
+        t = big.as_strided(x.shape, (1 << 22, 128, 1), 512 * i)
+        t.copy_(dev(x, DT[dt]))
+        far.append(t)
+    out = S.saki_attend_prompt(*far, ints(cu))
+    assert torch.equal(out, S.saki_attend_prompt(*(dev(x, DT[dt]) for x in (q, k, v)), ints(cu)))
+    check(out, q, k, v, cu, dt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_attend_prompt_captured_and_replayed(dt):
+    """In a graph, replayed with other offsets and inputs and eager work between."""
+    T, H_q, H_kv = 400, 8, 2
+    q, k, v = (dev(x, DT[dt]) for x in make(T, H_q, H_kv, dt, 14))
+    cu, out = ints([0, 100, 400]), torch.zeros(T, H_q, 128, dtype=DT[dt], device=DEV)
+    ws = torch.empty(S.saki_attend_prompt_workspace_bytes(dt, T, 2, H_kv), dtype=torch.uint8, device=DEV)
+    S.saki_attend_prompt(q, k, v, cu, out=out, ws=ws)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        S.saki_attend_prompt(q, k, v, cu, out=out, ws=ws)
+    rng = np.random.default_rng(15)
+    for i in range(5):
+        for t in (q, k, v):
+            t.copy_(dev(rng.standard_normal(t.shape), DT[dt]))
+        cu.copy_(ints([0, int(rng.integers(0, 400)), 400]))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, S.saki_attend_prompt(q, k, v, cu)), i

@@ -441,3 +441,109 @@ def test_step_captured_and_replayed():
             assert torch.equal(s[name], e[name]), (i, name)
         for a, b in zip(s["cache"], e["cache"]):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+
+
+# ---------------------------------------------------------------- large arrays, calls at once
+
+def test_offsets_past_32_bits():
+    """Blocks beyond 4 GiB of a cache, token rows more than 4 GiB apart: writes,
+    both attentions and the rotation."""
+    rng = np.random.default_rng(30)
+    H, n_blocks = 8, 1 + (5 << 30) // (8 * 8192)
+    kc = torch.zeros(n_blocks, H, 64, 128, dtype=F8, device=DEV)
+    vc = torch.zeros(n_blocks, H, 64, 128, dtype=F8, device=DEV)
+    sc = torch.zeros(n_blocks, H, 2, device=DEV)
+    ids = [n_blocks - 1, 3, n_blocks - 2]
+    slots = [ids[t // 64] * 64 + t % 64 for t in range(150)]
+    k, v = (rng.standard_normal((150, H, 128)) for _ in range(2))
+    S.saki_cache_write(dev(k), dev(v), ints(slots), kc, vc, sc)
+    near = [64 * i + t for i in range(3) for t in range(64)][:150]
+    wk, sk = O.cache_write(dev(k).double().cpu().numpy(), near, np.zeros((3, H, 64, 128)), np.zeros((3, H)))
+    wv, sv = O.cache_write(dev(v).double().cpu().numpy(), near, np.zeros((3, H, 64, 128)), np.zeros((3, H)))
+    for i, b in enumerate(ids):
+        np.testing.assert_array_equal(host(kc[b].float()), wk[i])
+        np.testing.assert_array_equal(host(vc[b].float()), wv[i])
+    q = rounded(rng.standard_normal((1, 2 * H, 1, 128)), "f32")
+    scales = np.stack([sk, sv], -1)
+    for idx in (None, np.tile(np.arange(0, 150, 3), (1, 2 * H, 1, 1))):
+        for wide in (0, 60):  # both ways of dividing the work
+            tab = ints([ids + [-1] * wide])
+            out = S.saki_cache_attend(dev(q), kc, vc, sc, tab, ints([150]), top_idx=None if idx is None else ints(idx))
+            want, mass, size = O.cache_attend(q, wk, wv, scales, [[0, 1, 2]], [150], idx)
+            assert np.all(np.abs(host(out) - want) <= attention_bound(want, mass, size, 150, "f32"))
+    del kc, vc
+    x = torch.zeros(3, (3 << 30) // 128, 128, dtype=torch.bfloat16, device=DEV)[:, :2]  # rows 6 GiB apart
+    y = rounded(rng.standard_normal((3, 2, 128)), "bf16")
+    x.copy_(dev(y, torch.bfloat16))
+    pos = ints([1, 70000, 5])
+    want = S.saki_rope(dev(y, torch.bfloat16), None, pos)[0]
+    S.saki_rope(x, None, pos, q_out=x)
+    assert torch.equal(x, want)
+
+
+def test_calls_at_once_on_two_streams():
+    """Two batches, each with its own workspace, interleaved on two streams."""
+    lens = [[3000, 100, 2500], [2100, 2900, 64]]
+    runs = []
+    for i in range(2):
+        q, codes, scales, (k, v, s), tab = attend_case(lens[i], 8, 2, 1, "f32", seed=i)
+        args = (dev(q), k, v, s, ints(tab), ints(lens[i]))
+        ws = torch.empty(S.saki_cache_attend_workspace_bytes(3, 8, 2, 1, tab.shape[1]), dtype=torch.uint8, device=DEV)
+        runs.append((args, ws, S.saki_cache_attend(*args), torch.empty_like(args[0]), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for args, ws, want, out, stream in runs:
+            S.saki_cache_attend(*args, out=out, ws=ws, stream=stream)
+    torch.cuda.synchronize()
+    for args, ws, want, out, stream in runs:
+        assert torch.equal(out, want)
+
+
+def test_arguments_of_other_kinds_are_refused():
+    """Types, shapes, strides and devices that the calls do not take."""
+    k = torch.zeros(4, 2, 64, 128, dtype=F8, device=DEV)
+    s = torch.zeros(4, 2, 2, device=DEV)
+    x = torch.zeros(5, 2, 128, device=DEV)
+    i5, tab, lens = ints(range(5)), ints([[0, 1]]), ints([70])
+    q = torch.zeros(1, 4, 1, 128, device=DEV)
+    for call in (
+            lambda: S.saki_cache_write(x.half(), x.half(), i5, k, k.clone(), s),
+            lambda: S.saki_cache_write(x, x.bfloat16(), i5, k, k.clone(), s),
+            lambda: S.saki_cache_write(x, x, i5[:4], k, k.clone(), s),
+            lambda: S.saki_cache_write(x, x, i5.long(), k, k.clone(), s),
+            lambda: S.saki_cache_write(x, x, i5.cpu(), k, k.clone(), s),
+            lambda: S.saki_cache_write(x.transpose(0, 1), x, i5, k, k.clone(), s),
+            lambda: S.saki_cache_write(x, x, i5, k.view(torch.uint8), k.clone(), s),
+            lambda: S.saki_cache_write(x, x, i5, k[:, :, ::2], k.clone(), s),
+            lambda: S.saki_cache_write(x, x, i5, k, k[:3], s),
+            lambda: S.saki_cache_write(x, x, i5, k, k.clone(), s.double()),
+            lambda: S.saki_cache_write(x, x, i5, k, k.clone(), s[:, :1]),
+            lambda: S.saki_cache_attend(q, k, k, s, tab[0], lens),
+            lambda: S.saki_cache_attend(q, k, k, s, tab, ints([70, 1])),
+            lambda: S.saki_cache_attend(q[:, :, :, :64], k, k, s, tab, lens),
+            lambda: S.saki_cache_attend(q, k, k, s, tab, lens, top_idx=ints([[[[0]]]])),
+            lambda: S.saki_cache_attend(q, k, k, s, tab, lens, out=q.bfloat16()),
+            lambda: S.saki_cache_attend(q.transpose(1, 2).expand(1, 4, 4, 128).transpose(1, 2), k, k, s, tab, lens),
+            lambda: S.saki_rope(x, x[:4], i5),
+            lambda: S.saki_rope(x, x, i5[:3]),
+            lambda: S.saki_rope(x, x, ints([[1] * 5] * 2)),
+            lambda: S.saki_rope(x, x, i5, q_out=x.flip(2)[:, :, ::2]),
+            lambda: S.saki_rope(x.expand(5, 2, 128).as_strided((5, 2, 128), (0, 128, 1)), x, i5),
+            lambda: S.saki_block_tables(lens, lens, i5, tab, i5, i5[:3]),
+            lambda: S.saki_block_tables(lens, lens, i5, tab.long(), i5, i5),
+            lambda: S.saki_attend_prompt(x, x, x, lens[:0]),
+            lambda: S.saki_attend_prompt(x, x[:, :1], x, ints([0, 5])),
+    ):
+        with pytest.raises(ValueError):
+            call()
+    for call, status in (
+            (lambda: S.saki_rope(x, x, i5, sections=(63,)), -1),
+            (lambda: S.saki_rope(torch.zeros(5 * 2 * 128 + 1, device=DEV)[1:].view(5, 2, 128), x, i5), -1),
+            (lambda: S.saki_rope(x, x, i5, rope_theta=0.0), -1),
+            (lambda: S.saki_cache_attend(torch.zeros(1, 3, 1, 128, device=DEV), k, k, s, tab, lens), -1),
+            (lambda: S.saki_cache_attend(torch.zeros(1, 2, 17, 128, device=DEV), k, k, s, tab, lens), -2),
+            (lambda: S.saki_block_tables(lens, ints([1]), i5, tab, ints([0]), ints([0]), lens=lens), -1),
+    ):
+        with pytest.raises(S.SakiError) as e:
+            call()
+        assert e.value.status == status

@@ -40,6 +40,7 @@ def test_rope(lib, kw, status):
     assert change(lib.saki_rope, good, ROPE, **kw) == status
 
 
+A = [C.c_void_p(0x1000 * (i + 1)) for i in range(9)]  # arrays apart from one another
 TABLES = "ctx new B free n_free tables max_blocks slots pos T cu lens counts stream".split()
 
 
@@ -48,9 +49,12 @@ TABLES = "ctx new B free n_free tables max_blocks slots pos T cu lens counts str
     (dict(new=None), ARG), (dict(free=None), ARG), (dict(tables=None), ARG), (dict(slots=None), ARG),
     (dict(pos=None), ARG), (dict(cu=None), ARG), (dict(lens=None), ARG), (dict(counts=None), ARG),
     (dict(max_blocks=1 << 25), UNSUP),
+    # outputs that overlap inputs: the lengths updated in place, a part of the free list
+    (dict(lens=A[0]), ARG), (dict(lens=A[1]), ARG), (dict(cu=C.c_void_p(0x1000 - 8)), ARG),
+    (dict(slots=C.c_void_p(0x3000 + 32)), ARG), (dict(tables=C.c_void_p(0x3000 - 28)), ARG), (dict(counts=A[0]), ARG),
 ])
 def test_block_tables(lib, kw, status):
-    good = [P, P, 2, P, 9, P, 4, P, P, 7, P, P, P, None]
+    good = [A[0], A[1], 2, A[2], 9, A[3], 4, A[4], A[5], 7, A[6], A[7], A[8], None]
     assert change(lib.saki_block_tables, good, TABLES, **kw) == status
 
 
