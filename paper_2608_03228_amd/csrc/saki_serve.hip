@@ -541,6 +541,25 @@ constexpr int kPartFloats = kPartRows * kHeadDim + 2 * kPartRows;  // sums, maxi
 constexpr int kMinPiece = 4;                                       // tiles a work-group takes at least
 constexpr int kAttendGroups = 512;                                 // two a CU
 
+// Tiles of fewer than 64 requests, one a lane: its own, the sum up to it, and
+// all (below 2^31, as a table has fewer than 2^25 blocks).
+struct Sums {
+  int mine, upto, total;
+};
+__device__ __forceinline__ Sums wave_sums(const CacheArgs& a) {
+  const int lane = threadIdx.x % kWave;
+  Sums s;
+  s.mine = lane < a.B ? tiles_of(a.lens[lane], a.max_blocks) : 0;
+  s.upto = s.mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int up = __shfl_up(s.upto, d);
+    if (lane >= d) s.upto += up;
+  }
+  s.total = __builtin_amdgcn_readlane(s.upto, kWave - 1);
+  return s;
+}
+
 // Where a work-group's share of the tiles begins.  All tiles of all (request,
 // KV head, 16-row block) pairs stand in one line, a request's pairs one after
 // another; group w takes [w * piece, (w + 1) * piece).
@@ -586,30 +605,38 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
   int b = blockIdx.x / pairs;
   if constexpr (SPLIT) {
     __shared__ long long part[4], found[2];
-    long long total = 0, mine = 0, upto = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 256) {
-      mine = b0 + tid < a.B ? (long long)tiles_of(a.lens[b0 + tid], a.max_blocks) * pairs : 0;
-      long long sum;
-      upto = group_scan(mine, part, &sum);
-      total += sum;
-    }
-    const Share sh = share_of(total, gridDim.x);
-    cur = sh.piece * blockIdx.x;
-    end = min(total, cur + sh.piece);
-    if (cur >= end) return;
-    for (int b0 = 0; b0 < a.B; b0 += 256) {
-      long long sum = total;
-      if (a.B > 256) {  // (else the sums above are the ones)
-        mine = b0 + tid < a.B ? (long long)tiles_of(a.lens[b0 + tid], a.max_blocks) * pairs : 0;
-        upto = base + group_scan(mine, part, &sum);
+    if (a.B < kWave) {  // every wave for itself
+      const Sums all = wave_sums(a);
+      const Share sh = share_of((long long)all.total * pairs, gridDim.x);
+      cur = sh.piece * blockIdx.x;
+      end = min(sh.total, cur + sh.piece);
+      if (cur >= end) return;
+      b = __builtin_ctzll(__ballot(cur < (long long)all.upto * pairs));
+      base = (long long)__builtin_amdgcn_readlane(all.upto - all.mine, b) * pairs;
+    } else {
+      long long total = 0;
+      for (int b0 = 0; b0 < a.B; b0 += 256) {
+        const int t = b0 + tid < a.B ? tiles_of(a.lens[b0 + tid], a.max_blocks) : 0;
+        long long sum;
+        group_scan((long long)t * pairs, part, &sum);
+        total += sum;
       }
-      if (cur < upto && cur >= upto - mine) found[0] = b0 + tid, found[1] = upto - mine;
-      base += sum;
-      if (cur < base) break;
+      const Share sh = share_of(total, gridDim.x);
+      cur = sh.piece * blockIdx.x;
+      end = min(total, cur + sh.piece);
+      if (cur >= end) return;
+      for (int b0 = 0; b0 < a.B; b0 += 256) {
+        const long long t = b0 + tid < a.B ? (long long)tiles_of(a.lens[b0 + tid], a.max_blocks) * pairs : 0;
+        long long sum;
+        const long long upto = base + group_scan(t, part, &sum);
+        if (cur < upto && cur >= upto - t) found[0] = b0 + tid, found[1] = upto - t;
+        base += sum;
+        if (cur < base) break;
+      }
+      __syncthreads();
+      b = (int)found[0];
+      base = found[1];
     }
-    __syncthreads();
-    b = (int)found[0];
-    base = found[1];
   }
 
   while (cur < end) {
@@ -801,18 +828,27 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int G = a.H_q / a.H_kv, R = G * a.Q, RB = (R + 15) / 16, pairs = a.H_kv * RB;
   const int b = blockIdx.x / pairs, pair = blockIdx.x % pairs;
-  long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 256) {
-    const int t = b0 + tid < a.B ? tiles_of(a.lens[b0 + tid], a.max_blocks) : 0;
-    long long sum;
-    const long long upto = group_scan((long long)t * pairs, part, &sum);
-    if (b0 + tid == b) s_base = total + upto - (long long)t * pairs;
-    total += sum;
+  long long total = 0, base;
+  int nt;
+  if (a.B < kWave) {
+    const Sums all = wave_sums(a);
+    total = (long long)all.total * pairs;
+    nt = __builtin_amdgcn_readlane(all.mine, b);
+    base = (long long)(__builtin_amdgcn_readlane(all.upto, b) - nt) * pairs;
+  } else {
+    for (int b0 = 0; b0 < a.B; b0 += 256) {
+      const int t = b0 + tid < a.B ? tiles_of(a.lens[b0 + tid], a.max_blocks) : 0;
+      long long sum;
+      const long long upto = group_scan((long long)t * pairs, part, &sum);
+      if (b0 + tid == b) s_base = total + upto - (long long)t * pairs;
+      total += sum;
+    }
+    __syncthreads();
+    nt = tiles_of(a.lens[b], a.max_blocks);
+    base = s_base;
   }
-  __syncthreads();
   const Share sh = share_of(total, groups);
-  const int nt = tiles_of(a.lens[b], a.max_blocks);
-  const long long from = s_base + (long long)nt * pair;
+  const long long from = base + (long long)nt * pair;
   const int w0 = (int)(from / sh.piece), w1 = nt ? (int)((from + nt - 1) / sh.piece) : w0;
   if (nt && w0 == w1) return;
   const int row = lane / 4;
