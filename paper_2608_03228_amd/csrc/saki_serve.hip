@@ -541,8 +541,8 @@ constexpr int kPartFloats = kPartRows * kHeadDim + 2 * kPartRows;  // sums, maxi
 constexpr int kMinPiece = 4;                                       // tiles a work-group takes at least
 constexpr int kAttendGroups = 512;                                 // two a CU
 
-// Tiles of fewer than 64 requests, one a lane: its own, the sum up to it, and
-// all (below 2^31, as a table has fewer than 2^25 blocks).
+// Tiles of up to 64 requests, one a lane: its own, the sum up to it, and all
+// (below 2^31, as a table has fewer than 2^25 - 1 blocks).
 struct Sums {
   int mine, upto, total;
 };
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
   int b = blockIdx.x / pairs;
   if constexpr (SPLIT) {
     __shared__ long long part[4], found[2];
-    if (a.B < kWave) {  // every wave for itself
+    if (a.B <= kWave) {  // every wave for itself
       const Sums all = wave_sums(a);
       const Share sh = share_of((long long)all.total * pairs, gridDim.x);
       cur = sh.piece * blockIdx.x;
@@ -830,7 +830,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups
   const int b = blockIdx.x / pairs, pair = blockIdx.x % pairs;
   long long total = 0, base;
   int nt;
-  if (a.B < kWave) {
+  if (a.B <= kWave) {
     const Sums all = wave_sums(a);
     total = (long long)all.total * pairs;
     nt = __builtin_amdgcn_readlane(all.mine, b);
@@ -1112,14 +1112,18 @@ namespace {
 // Whether a work-group takes a whole pair: the lengths are read on the device,
 // so the tables' width has to bound a group's time.  us (bf16, 32 / 8 heads),
 // split and joined / whole pairs, for requests of the full width:
-//               4 tiles      8          16          32          64
-//    1 request   9.3 / 5.7  10.5 / 7.6  10.7 / 10.8  11.0 / 17.2  11.9 / 29.6
-//    8           9.7 / 5.8  10.9 / 7.7  11.2 / 10.9  14.7 / 18.8
-//   64          16.9 / 8.5  22.4 / 14.5 32.4 / 24.0  52.2 / 43.3
-//  256          49.8 / 26.1             119 / 101
-// (512 pairs and more fill the GPU without being split, up to the width where
-// one long request among short ones would keep a group alone at work).
-bool whole_better(long long pairs, int max_blocks) { return max_blocks <= (pairs >= 512 ? 32 : 16); }
+//                4 tiles       8            12           16           32           64
+//    1 request   8.1 / 5.7    9.4 / 7.6    9.3 / 9.2    9.5 / 10.8  10.0 / 17.2  10.8 / 29.6
+//    8           8.4 / 5.8    9.7 / 7.7    9.8 / 9.3   10.0 / 10.9  13.2 / 18.8
+//   16                                                 13.5 / 12.2
+//   32                       14.2 / 8.5                20.8 / 14.7  30.6 / 23.3
+//   64          12.7 / 8.2   18.7 / 14.3               29.1 / 24.7  49.3 / 44.0   106 / 99
+//  256          34.1 / 26.2                             108 / 100    193 / 192
+// (many pairs fill the GPU without being split, up to the width where one long
+// request among short ones would keep its groups at work alone for long).
+bool whole_better(long long pairs, int max_blocks) {
+  return max_blocks <= (pairs >= 512 ? 64 : pairs >= 256 ? 32 : pairs >= 128 ? 16 : 12);
+}
 
 }  // namespace
 
@@ -1175,7 +1179,7 @@ int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q,
   const size_t need = saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, 0);
   if (!ws || ws_bytes < need || !aligned(ws, 16)) return SAKI_ERR_WORKSPACE;
   const int groups = (int)(need / (2 * kPartFloats * sizeof(float)));
-  const dim3 join((unsigned)pairs, pairs >= 256 ? 1 : kHeadDim / 16);
+  const dim3 join((unsigned)pairs, pairs > 256 ? 1 : kHeadDim / 16);
   if (dtype == SAKI_F32) {
     hipLaunchKernelGGL((cache_attend_kernel<true, true>), dim3(groups), dim3(256), 0, s, a, q, out, (float*)ws);
     if (!launched()) return SAKI_ERR_HIP;

@@ -286,13 +286,13 @@ def check_attend(case, lens, dt, top_idx=None, **kw):
     ([0], 2, 1, 3), ([1000], 32, 8, 1), ([300, 1, 640, 129], 12, 1, 4), ([3, 200], 5, 5, 16),
     ([2], 4, 2, 16), ([700, 699], 17, 1, 1), ([-4, 70], 2, 1, 2), ([1500, 300], 4, 1, 1),
 ])
-@pytest.mark.parametrize("rows", [None, 40])  # narrow tables: a work-group per pair; wide ones: shares, joined
+@pytest.mark.parametrize("rows", [None, 70])  # narrow tables: a work-group per pair; wide ones: shares, joined
 def test_cache_attend(rows, lens, H_q, H_kv, Q, dt):
     check_attend(attend_case(lens, H_q, H_kv, Q, dt, rows), lens, dt)
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [15, 40])
+@pytest.mark.parametrize("rows", [15, 70])
 def test_cache_attend_many_requests(rows, dt):
     """More requests than one scan step takes, most of them short."""
     rng = np.random.default_rng(0)
@@ -339,7 +339,7 @@ def test_cache_attend_peaked_rows(top_idx):
 def test_cache_attend_is_the_same_every_time_and_on_another_stream():
     lens = [3000, 10, 700, 2500]
     q, codes, scales, (k, v, s), tab = attend_case(lens, 28, 4, 1, "bf16")
-    assert tab.shape[1] > 32  # shares and their join
+    assert tab.shape[1] > 16  # shares and their join
     args = (dev(q, torch.bfloat16), k, v, s, ints(tab), ints(lens))
     first = S.saki_cache_attend(*args)
     side = torch.cuda.Stream()
@@ -466,7 +466,7 @@ def test_offsets_past_32_bits():
     q = rounded(rng.standard_normal((1, 2 * H, 1, 128)), "f32")
     scales = np.stack([sk, sv], -1)
     for idx in (None, np.tile(np.arange(0, 150, 3), (1, 2 * H, 1, 1))):
-        for wide in (0, 60):  # both ways of dividing the work
+        for wide in (0, 80):  # both ways of dividing the work
             tab = ints([ids + [-1] * wide])
             out = S.saki_cache_attend(dev(q), kc, vc, sc, tab, ints([150]), top_idx=None if idx is None else ints(idx))
             want, mass, size = O.cache_attend(q, wk, wv, scales, [[0, 1, 2]], [150], idx)
