@@ -14,6 +14,10 @@
  *   saki_recall        GPU: exact float64 q.k top-k and its overlap with a
  *                      candidate top-k (recall of the true top-k, Sec. 3)
  *
+ * Beside the index: saki_attend (attention over its lists) and what a server
+ * runs around it (saki_rope, saki_block_tables, saki_cache_write,
+ * saki_cache_attend, saki_attend_prompt; "Serving around the index" below).
+ *
  * Conventions shared by every entry point
  *   - Return value: SAKI_OK (0) or a negative saki_status; nothing throws.
  *   - Arrays are dense, row-major, and owned by the caller.  "device" means
