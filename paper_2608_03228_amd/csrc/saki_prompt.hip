@@ -87,6 +87,22 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
+// out_t = sum_u p_u v_u over the keys u <= t of a prompt.  A work-group takes 128
+// rows (32 a wave) and reads the keys and values up to its last token in tiles
+// of 64, staged into LDS by direct loads a tile ahead; 64 KB a group, two groups
+// a CU, whose waves fill each other's pauses.  S^T = K Q^T leaves a lane with
+// scores of one row (half of a tile's keys; lane + 32 has the others), so the
+// softmax is in registers but for one exchange, and its weights, rounded to
+// bf16, are at once the operand of O^T = V^T P^T, whose other operand the
+// transposing LDS reads form.  Key pieces are staged rotated by their row, so
+// that neither read meets bank conflicts (0 counted).  The blocks with most keys
+// come first in the launch.
+// KS = 2: 64 rows, and two waves share a row's keys, 32 of each tile; their
+// sums meet at the end (see halves_better).
+// Bound by power and the MFMA: 0.99-1.06 PFLOP/s at 8,192 tokens of 32 / 8
+// heads depending on the card (a large bf16 matrix product reaches 1.15), the
+// MFMA 55% busy at a clock of 1.8 GHz.  Raising the waves' priority around the
+// products or the softmax changed nothing.
 template <int KS>
 __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
   constexpr int kBlockRows = kRows / KS;
@@ -265,7 +281,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
 // 2^e - hi), where 2^e brings the largest element of a tile (of a query's row)
 // to [2^14, 2^15).  What hi and lo leave is below 2^-22 |x|, or 2^-39 of that
 // largest element, and a product is hi hi + lo hi + hi lo, all sums in float32:
-// three fp16 products in place of one at an eighth of their rate.
+// three fp16 products in place of one at an eighth of their rate.  4,096 tokens
+// of 28 / 4 heads: 10.7 us for the split and 350-390 for the attention (310-340
+// TFLOP/s, the MFMA 63% busy); on the float32 MFMA it took 1,237 us.
 
 constexpr int kSplitKeys = 32;
 constexpr int kSplitTile = 4 * kSplitKeys * kHeadDim * 2;  // bytes: keys hi, lo, values hi, lo
@@ -355,6 +373,8 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
   }
 }
 
+// As prompt_attend_kernel, on tiles of 32 keys in parts; with KS = 2 a step
+// stages two tiles and each half of the waves takes one.
 template <int KS>
 __global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
                                                                    const int2* __restrict__ exps) {

@@ -108,7 +108,9 @@ __device__ __forceinline__ void sin_cos_turns(double turns, float* s, float* c) 
 // pos[axis(m)][t] * theta^(-2m/d).  One wave per token and share of its heads;
 // a lane holds the same pairs of every head it visits, so that a token's sines
 // and cosines are formed once per wave.  Each lane reads both halves of its
-// pairs before it writes them: the outputs may be the inputs.  HBM bound.
+// pairs before it writes them: the outputs may be the inputs.  HBM bound: 16,384
+// float32 tokens of 28 + 4 heads in 100 us, 5.4 TB/s; 64 bf16 tokens of 32 + 8
+// heads, a few loads deep, in 3.6.
 constexpr int kRopeWaves = 4;
 constexpr int kRopeAhead = 4;  // heads a lane has in flight
 template <typename T>
@@ -206,6 +208,7 @@ __device__ __forceinline__ int find_last(const long long* at, int n, long long x
 // and fills its share of the tokens and of the new table entries, so that one
 // launch does and nothing waits for another group: an entry of the tables is
 // read only where it was there before, and written only where it was not.
+// Latency bound: 5.0 us for 64 requests of one token, 6.2 for 512 with 131,000.
 constexpr int kTableChunk = 1024;
 __global__ __launch_bounds__(256) void block_tables_kernel(
     const int* __restrict__ ctx, const int* __restrict__ fresh, int B, const int* __restrict__ free_blocks,
@@ -327,8 +330,9 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 // is the least power of two that covers the run, and, where the block holds
 // tokens before the run, no less than it was; if it grew, the codes before the
 // run are moved to it.  Powers of two make that exact but for codes that become
-// subnormal, and codes times scale exact in bf16.  HBM bound on prompts, latency
-// on single tokens.
+// subnormal, and codes times scale exact in bf16.  HBM bound on prompts: 30,400
+// float32 tokens of 4 heads in 37 us, 4.3 TB/s (repeated on the same arrays 5.5);
+// latency on single tokens: 64 of 8 heads in 3.6.
 template <typename T>
 __global__ __launch_bounds__(256) void cache_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
                                                           size_t ld_k, size_t ld_v, int n_tokens, int window,
@@ -588,7 +592,11 @@ __device__ __forceinline__ Share share_of(long long total, int groups) {
 // registers; dims 8 m .. 8 m + 7 of lane m are the rows m of eight products.
 // The codes are exact in bf16; queries (float32: three terms) and weights (two
 // terms, three for float32 output) are split so that nothing but the output is
-// rounded to bf16.  HBM bound: 16 KB a tile.
+// rounded to bf16.  HBM bound, 16 KB a tile: 8 requests of up to 131,072 keys in
+// 4 heads in 110 us, 5.35 TB/s of 590 MB fetched.  A request of 4,001 keys in 8
+// heads takes 9.9 us, and the join 4.1: a chain of reads (lengths, table, codes)
+// with a tile a wave behind it.  Holding the next tile's codes in registers
+// (241 of them) did not shorten either, 14.2 us against 13.5 for the step.
 //
 // Without SPLIT a work-group takes one whole pair: no share to find, no
 // workspace and no join (see whole_better).
@@ -896,7 +904,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups
 
 // Attention over listed keys: one wave per (request, head, query) row.  Lane e
 // looks up entry e; eight lanes then read one key's or value's 128 bytes, eight
-// entries at a time, all in flight together.  Latency bound: list, table, codes.
+// entries at a time, all in flight together.  Latency bound: list, table, codes
+// (8 requests x 32 heads over 131,072 keys: 8.7 us for 6.7 MB).
 template <bool F32>
 __global__ __launch_bounds__(256) void cache_lists_kernel(CacheArgs a, const void* __restrict__ q,
                                                           const int* __restrict__ top_idx, int k, size_t rows,
