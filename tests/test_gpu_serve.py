@@ -547,3 +547,43 @@ def test_arguments_of_other_kinds_are_refused():
         with pytest.raises(S.SakiError) as e:
             call()
         assert e.value.status == status
+
+
+# ---------------------------------------------------------------- beside the index
+
+def test_index_lists_read_from_the_cache():
+    """The index's lists over the 8-bit cache against saki_attend over the exact
+    keys: codes from unrotated keys, rotated keys in the cache."""
+    import workloads as W
+    N, H_q, H_kv, B = 1500, 8, 2, 2
+    spec = W.SPECS["decode_1m"].with_(N=N, H_q=H_q, H_kv=H_kv, batch=B, Q=1)
+    inp = W.make_layer(spec, with_values=True)
+    cal = S.saki_calibrate(inp["q_cal"], inp["k_cal"], 32)
+    keys, vals, q = dev(inp["keys"]), dev(inp["values"]), dev(inp["queries"])
+    index = S.saki_build_index(keys, dev(cal["B_k"]), dev(cal["mu"]), 32, "bf16", H_q)
+    idx, _ = S.saki_score_topk(index, "bf16", q, dev(cal["B_q"]), dev(cal["mu"]), H_kv, N, N, 32)
+    exact = host(S.saki_attend(vals, q, idx, N, keys=keys))
+    # the same tokens through tables, rotation and the cache
+    rows = -(-N // 64)
+    free = ints(np.random.default_rng(1).permutation(B * rows))
+    slots, pos = (torch.empty(B * N, dtype=torch.int32, device=DEV) for _ in range(2))
+    tab = torch.full((B, rows), -1, dtype=torch.int32, device=DEV)
+    tab, slots, pos, cu, lens, counts = S.saki_block_tables(ints([0] * B), ints([N] * B), free, tab, slots, pos)
+    k = keys.transpose(1, 2).reshape(B * N, H_kv, 128).contiguous()
+    v = vals.transpose(1, 2).reshape(B * N, H_kv, 128).contiguous()
+    _, kr = S.saki_rope(k[:, :1], k, pos)
+    cache = (torch.zeros(B * rows, H_kv, 64, 128, dtype=F8, device=DEV),
+             torch.zeros(B * rows, H_kv, 64, 128, dtype=F8, device=DEV), torch.zeros(B * rows, H_kv, 2, device=DEV))
+    S.saki_cache_write(kr, v, slots, *cache)
+    qr, _ = S.saki_rope(q.view(B, H_q, 128), None, ints([N - 1] * B))
+    got = host(S.saki_cache_attend(qr.view(B, H_q, 1, 128), *cache, tab, lens, top_idx=idx))
+    # exactly the attention of what the cache holds ...
+    codes = [host(c.float()) for c in cache[:2]]
+    want, mass, size = O.cache_attend(host(qr)[:, :, None], codes[0], codes[1], host(cache[2]), host(tab), [N] * B,
+                                      host(idx))
+    assert np.all(np.abs(got - want) <= attention_bound(want, mass, size, N, "f32"))
+    # ... which holds keys and values to half an E4M3 step, 2^-4 of an element:
+    # a score is off by 2^-4 size at most (and the rotation's 9 u), a value by 2^-4
+    e = 2 * (2.0 ** -4 * size * 17 / 15)[..., None]
+    top = np.abs(host(vals)).max()
+    assert np.all(np.abs(got - exact) <= np.minimum(np.expm1(e), 2) * top + (2.0 ** -4 + 1e-4) * top)
