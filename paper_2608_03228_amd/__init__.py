@@ -1,8 +1,9 @@
 """SAKI (score-aware low-rank key indexing) retrieval-index path for MI355X.
 
 The compute lives in libsaki.so (host float64 calibration + gfx950 HIP
-kernels, C ABI in include/saki.h); ``paper_2608_03228_amd.saki`` is its thin
-ctypes binding.  Build with ``python -m paper_2608_03228_amd.build``.
+kernels, C ABI in include/saki.h): the index, and serving around it (rotary
+positions, block tables, an 8-bit paged cache, its attention and that of whole
+prompts).  ``paper_2608_03228_amd.saki`` is its thin ctypes binding.  Build with ``python -m paper_2608_03228_amd.build``.
 """
 from . import saki  # noqa: F401
 from .saki import (  # noqa: F401

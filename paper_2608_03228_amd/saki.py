@@ -5,7 +5,8 @@ and does no arithmetic of its own: host functions take and return numpy
 arrays, GPU functions take torch CUDA tensors (torch supplies device memory
 and the current HIP stream) and enqueue the library's kernels on that
 stream.  If the shared library is missing, every call raises: there is no
-fallback path.
+fallback path.  The serving calls pass their arguments through _saki_args, a
+module in C++ that checks tensors in less time than Python takes.
 """
 from __future__ import annotations
 
@@ -487,6 +488,12 @@ def _of_floats(t, dims, name):
     return shape, dt, code
 
 
+def _heads(t, name):
+    if not isinstance(t, _torch_mod.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a [T, H_kv, d] tensor")
+    return t.shape[1]
+
+
 def _cache_arrays(k_cache, v_cache, scales, dev):
     """-> pointers, n_blocks, H_kv, d"""
     torch = _torch()
@@ -549,7 +556,7 @@ def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse:
     H_kv = ldk = ldko = 0
     kp = ko = None
     if k is not None:
-        H_kv = k.shape[1]
+        H_kv = _heads(k, "k")
         kshape = (T, H_kv, d)
         kp, ldk = _rows(k, dt, kshape, dev, "k")
         if k_out is None:
@@ -671,7 +678,7 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
     shape, dt, code = _of_floats(q, 3, "q")
     torch, dev, cur = _current()
     T, H_q, d = shape
-    H_kv = k.shape[1]
+    H_kv = _heads(k, "k")
     kshape = (T, H_kv, d)
     qp, ldq = _rows(q, dt, shape, dev, "q")
     kp, ldk = _rows(k, dt, kshape, dev, "k")

@@ -138,3 +138,24 @@ def test_binding_refuses_host_tensors():
         S.saki_cache_attend(torch.zeros(1, 4, 1, 128), c, c, s, i[None], i[:1])
     with pytest.raises(ValueError):
         S.saki_attend_prompt(x, x, x, i)
+
+
+def test_argument_module_checks_counts_and_ranges():
+    m = S._args()
+    with pytest.raises(TypeError):
+        m.saki_block_tables(1, 2)
+    with pytest.raises(OverflowError):
+        m.saki_cache_attend_workspace_bytes(1 << 40, 4, 1, 1, 1, 0)
+    with pytest.raises(OverflowError):
+        m.saki_rope(0, 0, 1, 5, 4, 2, 128, -1, 256, 0, 1, 0, 1e4, 0, 0, 0, 512, 256, None)
+    with pytest.raises(TypeError):
+        m.saki_cache_attend_workspace_bytes("1", 4, 1, 1, 1, 0)
+    assert m.saki_cache_attend_workspace_bytes(1, 4, 1, 1, 100, 0) == S.saki_cache_attend_workspace_bytes(1, 4, 1, 1, 100)
+    x = torch.zeros(2, 3)
+    for f in (m.array, m.rows):
+        with pytest.raises(ValueError, match="must be a CUDA"):
+            f(x, torch.float32, (2, 3), 0, "x")
+        with pytest.raises(ValueError, match="must be a CUDA"):
+            f(None, torch.float32, (2, 3), 0, "x")
+        with pytest.raises(TypeError):
+            f(x, torch.float32)
