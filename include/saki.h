@@ -403,8 +403,9 @@ int saki_rope(const void* q, const void* k, int dtype, int T, int H_q, int H_kv,
  *   lens       device int [B] out: tokens that have a block, ctx and new
  *   counts     device int [2] out: blocks taken (the first of the list), blocks lacking
  * Of more than T tokens only the first T have slots and pos; with fewer, the
- * rest of the two arrays is left as it was.  No output overlaps ctx_lens,
- * new_lens or free_blocks (SAKI_ERR_ARG).
+ * rest of slots is -1 and of pos 0, so that a step of a fixed size (a captured
+ * one) writes nothing for it.  No output overlaps ctx_lens, new_lens or
+ * free_blocks (SAKI_ERR_ARG).
  */
 int saki_block_tables(const int* ctx_lens, const int* new_lens, int B, const int* free_blocks,
                       int n_free, int* tables, int max_blocks, int* slots, int* pos, int T,

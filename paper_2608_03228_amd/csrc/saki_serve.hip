@@ -282,6 +282,7 @@ __global__ __launch_bounds__(256) void block_tables_kernel(
     want0 = want1;
     __syncthreads();  // the chunk's arrays are read
   }
+  for (; t < T; t += stride) slots[t] = -1, pos[t] = 0;  // no token of any request
   if (blockIdx.x == 0) {
     long long lacking;
     group_scan(lack, part, &lacking);

@@ -129,9 +129,9 @@ def tables_case(ctx, new, n_free, rows, T=None, seed=0):
     got = [host(t) for t in S.saki_block_tables(ints(ctx), ints(new), ints(free), ints(tab), slots, pos)]
     m = min(n, T)
     np.testing.assert_array_equal(got[0], want[0])
-    for g, w in ((got[1], want[1]), (got[2], want[2])):
+    for g, w, rest in ((got[1], want[1], -1), (got[2], want[2], 0)):
         np.testing.assert_array_equal(g[:m], w[:m])
-        assert (g[m:] == -77).all()
+        assert (g[m:] == rest).all()
     for g, w in zip(got[3:], want[3:]):
         np.testing.assert_array_equal(g, w)
 
@@ -547,6 +547,51 @@ def test_arguments_of_other_kinds_are_refused():
         with pytest.raises(S.SakiError) as e:
             call()
         assert e.value.status == status
+
+
+def test_step_of_a_fixed_size_with_fewer_tokens():
+    """A captured step for 4 requests and 8 tokens, replayed with fewer of both:
+    what stands behind the last token is neither written to the cache nor read."""
+    rng = np.random.default_rng(31)
+    H_q, H_kv, B, T = 4, 2, 4, 8
+    s, codes, scales, tab, free = step_state([70, 0, 10, 130], H_q, H_kv, "f32", rng)
+    z = lambda *n, d=torch.int32: torch.zeros(n, dtype=d, device=DEV)  # noqa: E731
+    s.update(slots=ints([5] * T), pos=ints([9] * T), q=z(T, H_q, 128, d=torch.float32),
+             k=z(T, H_kv, 128, d=torch.float32))
+    x = z(T, H_q + 2 * H_kv, 128, d=torch.float32)
+
+    def run():
+        S.saki_block_tables(s["ctx"], s["new"], s["free"], s["tab"], s["slots"], s["pos"], cu=s["cu"], lens=s["lens"],
+                            counts=s["counts"])
+        S.saki_rope(x[:, :H_q], x[:, H_q:H_q + H_kv], s["pos"], q_out=s["q"], k_out=s["k"])
+        S.saki_cache_write(s["k"], x[:, H_q + H_kv:], s["slots"], *s["cache"])
+
+    s["new"].zero_()
+    x.fill_(float("nan"))
+    before = [c.clone() for c in s["cache"]]
+    run()  # no token at all
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        run()
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, s["cache"]))
+    kc, sk = codes[0], scales[..., 0]
+    vc, sv = codes[1], scales[..., 1]
+    for new in ([1, 0, 1, 0], [0, 3, 0, 1], [0, 0, 0, 0], [2, 2, 2, 2]):
+        n = sum(new)
+        y = rounded(rng.standard_normal((n, H_q + 2 * H_kv, 128)), "f32")
+        x.fill_(float("nan"))
+        x[:n].copy_(dev(y))
+        s["new"].copy_(ints(new))
+        g.replay()
+        torch.cuda.synchronize()
+        wt, slots, pos, cu, lens, counts = O.block_tables(host(s["ctx"]), new, free, tab)
+        assert host(s["slots"]).tolist() == slots.tolist() + [-1] * (T - n)
+        k = host(s["k"])[:n]
+        kc, sk = O.cache_write(k, slots, kc, sk)
+        vc, sv = O.cache_write(y[:, H_q + H_kv:], slots, vc, sv)
+        np.testing.assert_array_equal(host(s["cache"][0].float()), kc)
+        np.testing.assert_array_equal(host(s["cache"][1].float()), vc)
 
 
 # ---------------------------------------------------------------- beside the index
