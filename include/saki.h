@@ -425,6 +425,7 @@ int saki_block_tables(const int* ctx_lens, const int* new_lens, int B, const int
  *            not specified); tokens with slots out of range are skipped, and
  *            what they hold has no effect
  *   k_cache, v_cache  device [n_blocks, H_kv, 64, d] bytes;  scales device float
+ *            (SAKI_ERR_ARG where they overlap)
  * Codes of other slots of the blocks, and other blocks, are left as they were.
  * T <= 2^26.
  */
@@ -451,7 +452,8 @@ size_t saki_cache_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int ma
  *   top_idx  device int [B, H_q, Q, k], k <= 64, or NULL with k = 0
  *   ws       device workspace of saki_cache_attend_workspace_bytes(...) (k = 0),
  *            16-byte aligned
- * The time goes by the lengths on the device; max_blocks only bounds the workspace.
+ * out overlaps no input.  The time goes by the lengths on the device; max_blocks
+ * bounds the workspace and, while it is small, says how the work is divided.
  */
 int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q, int d,
                       const void* k_cache, const void* v_cache, const float* scales,
@@ -476,7 +478,8 @@ size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv);
  *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v
  *           apart (ld up to 2^22)
  *   cu      device int [B + 1], ascending: prompt b is tokens [cu[b], cu[b+1])
- *   out     device [T, H_q, d], dense; tokens of no prompt are left as they were
+ *   out     device [T, H_q, d], dense, overlaps no input; tokens of no prompt are
+ *           left as they were
  *   ws      device workspace of saki_attend_prompt_workspace_bytes(...), 16-byte
  *           aligned (float32; bf16 needs none and ws may be NULL)
  */

@@ -1003,6 +1003,10 @@ bool rows_ok(const void* p, size_t ld, int H, int dtype) {
   return p && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld >= (size_t)H * kHeadDim &&
          ld * type_bytes(dtype) % 16 == 0 && ld <= ((size_t)1 << 40);
 }
+bool overlap(const void* p, size_t n, const void* q, size_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + m && b < a + n;
+}
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 constexpr int kMaxTokens = 1 << 26;  // a launch's threads fit 32 bits
@@ -1045,12 +1049,11 @@ int saki_rope(const void* q, const void* k, int dtype, int T, int H_q, int H_kv,
   if (H_q && (!rows_ok(q, ld_q, H_q, dtype) || !rows_ok(q_out, ld_q_out, H_q, dtype))) return SAKI_ERR_ARG;
   if (H_kv && (!rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(k_out, ld_k_out, H_kv, dtype))) return SAKI_ERR_ARG;
   Turns turns;
-  double lo[8], hi[8];
-  for (int i = 0; i < 8; ++i) {
-    lo[i] = std::pow((double)rope_theta, -2.0 * i / d);
-    hi[i] = std::pow((double)rope_theta, -16.0 * i / d) * 0.15915494309189533577;
-  }
-  for (int m = 0; m < d / 2; ++m) turns.f[m] = hi[m / 8] * lo[m % 8];
+  // powers of theta^(-2/d) by products of 64-bit significands: each within half
+  // a unit of float64's last place and 2^-56
+  const long double r = std::pow((long double)rope_theta, -2.0L / d);
+  long double f = 0.15915494309189533576888L;
+  for (int m = 0; m < d / 2; ++m, f *= r) turns.f[m] = (double)f;
   // heads that a wave visits at once; a token's heads are split over up to that
   // many waves while there are few tokens
   const int at_once = dtype == SAKI_F32 ? 4 : 8;
@@ -1084,7 +1087,7 @@ int saki_block_tables(const int* ctx_lens, const int* new_lens, int B, const int
   const size_t to_n[6] = {(size_t)B * max_blocks, (size_t)T, (size_t)T, (size_t)B + 1, (size_t)B, 2};
   for (int i = 0; i < 3; ++i)  // (a group may write before another has read)
     for (int j = 0; j < 6; ++j)
-      if (in[i] < to[j] + to_n[j] && to[j] < in[i] + in_n[i]) return SAKI_ERR_ARG;
+      if (overlap(in[i], in_n[i] * sizeof(int), to[j], to_n[j] * sizeof(int))) return SAKI_ERR_ARG;
   int groups = (T + 255) / 256;  // a token a thread: 512 x 256 tokens in 6.0 us, two 6.8, four 8.5
   groups = groups < 1 ? 1 : groups > 1024 ? 1024 : groups;
   hipLaunchKernelGGL(block_tables_kernel, dim3(groups), dim3(256), 0, reinterpret_cast<hipStream_t>(stream),
@@ -1101,6 +1104,10 @@ int saki_cache_write(const void* k, const void* v, int dtype, int T, int H_kv, i
   if (T == 0) return SAKI_OK;
   if (!slots || !rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(v, ld_v, H_kv, dtype)) return SAKI_ERR_ARG;
   if (n_blocks == 0) return SAKI_OK;  // no slot is within it
+  const size_t codes = (size_t)n_blocks * H_kv * kBlockBytes, n_scales = (size_t)n_blocks * H_kv * 2 * sizeof(float);
+  if (overlap(k_cache, codes, v_cache, codes) || overlap(k_cache, codes, scales, n_scales) ||
+      overlap(v_cache, codes, scales, n_scales))
+    return SAKI_ERR_ARG;
   // some 2,000 work-groups (twice as many: 4,000 tokens of 8 heads 10.1 us in place of 7.1)
   int window = 1;
   while (window < kWave && (long long)T * 2 * H_kv > 2048LL * window) window *= 2;

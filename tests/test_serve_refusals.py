@@ -67,9 +67,12 @@ WRITE = "k v dtype T H_kv d ld_k ld_v slots k_cache v_cache scales n_blocks stre
     (dict(n_blocks=1 << 24), UNSUP), (dict(k=None), ARG), (dict(v=ODD), ARG), (dict(slots=None), ARG),
     (dict(k_cache=None), ARG), (dict(v_cache=ODD), ARG), (dict(scales=None), ARG), (dict(scales=C.c_void_p(4100)), ARG),
     (dict(ld_k=255), ARG), (dict(ld_v=260), ARG),
+    # caches that overlap each other or their scales: 9 blocks of 2 heads are 0x24000 bytes
+    (dict(v_cache=C.c_void_p(0x100000)), ARG), (dict(v_cache=C.c_void_p(0x123ff0)), ARG),
+    (dict(scales=C.c_void_p(0x100010)), ARG), (dict(scales=C.c_void_p(0x1fff78)), ARG),
 ])
 def test_cache_write(lib, kw, status):
-    good = [P, P, 1, 5, 2, 128, 256, 256, P, P, P, P, 9, None]
+    good = [P, P, 1, 5, 2, 128, 256, 256, P, C.c_void_p(0x100000), C.c_void_p(0x200000), C.c_void_p(0x300000), 9, None]
     assert change(lib.saki_cache_write, good, WRITE, **kw) == status
 
 
