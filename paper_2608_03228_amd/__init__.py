@@ -8,8 +8,8 @@ prompts).  ``paper_2608_03228_amd.saki`` is its thin ctypes binding.  Build with
 from . import saki  # noqa: F401
 from .saki import (  # noqa: F401
     saki_attend, saki_attend_prompt, saki_attend_prompt_workspace_bytes, saki_block_tables,
-    saki_build_index, saki_cache_attend, saki_cache_attend_workspace_bytes, saki_cache_write, saki_calibrate, saki_index_bytes,
-    saki_index_export, saki_recall, saki_recall_workspace_bytes, saki_rope, saki_score_topk,
-    saki_score_topk_workspace_bytes, saki_status_string, saki_sym_eig, saki_version,
-    saki_weight_svd_factors,
+    saki_build_index, saki_cache_attend, saki_cache_attend_workspace_bytes, saki_cache_write,
+    saki_calibrate, saki_index_bytes, saki_index_export, saki_recall, saki_recall_workspace_bytes,
+    saki_rope, saki_score_topk, saki_score_topk_workspace_bytes, saki_status_string, saki_sym_eig,
+    saki_version, saki_weight_svd_factors,
 )
