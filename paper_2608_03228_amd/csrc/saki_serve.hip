@@ -549,12 +549,13 @@ constexpr int kAttendGroups = 512;                                 // two a CU
 // Tiles of up to 64 requests, one a lane: its own, the sum up to it, and all
 // (below 2^31, as a table has fewer than 2^25 - 1 blocks).
 struct Sums {
-  int mine, upto, total;
+  int len, mine, upto, total;
 };
 __device__ __forceinline__ Sums wave_sums(const CacheArgs& a) {
   const int lane = threadIdx.x % kWave;
   Sums s;
-  s.mine = lane < a.B ? tiles_of(a.lens[lane], a.max_blocks) : 0;
+  s.len = lane < a.B ? a.lens[lane] : 0;
+  s.mine = tiles_of(s.len, a.max_blocks);
   s.upto = s.mine;
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) {
@@ -611,7 +612,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
   const int G = a.H_q / a.H_kv, R = G * a.Q, RB = (R + 15) / 16, pairs = a.H_kv * RB;
 
   long long cur = 0, end = 1, base = 0;  // the tiles to take, the tiles before request b
-  int b = blockIdx.x / pairs;
+  int b = blockIdx.x / pairs, lens = 0;  // (lens: of request `lane` of up to 64)
   if constexpr (SPLIT) {
     __shared__ long long part[4], found[2];
     if (a.B <= kWave) {  // every wave for itself
@@ -622,6 +623,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
       if (cur >= end) return;
       b = __builtin_ctzll(__ballot(cur < (long long)all.upto * pairs));
       base = (long long)__builtin_amdgcn_readlane(all.upto - all.mine, b) * pairs;
+      lens = all.len;
     } else {
       long long total = 0;
       for (int b0 = 0; b0 < a.B; b0 += 256) {
@@ -649,7 +651,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
   }
 
   while (cur < end) {
-    const int len = a.lens[b], nt = tiles_of(len, a.max_blocks);
+    const int len = SPLIT && a.B <= kWave ? __builtin_amdgcn_readlane(lens, b) : a.lens[b];
+    const int nt = tiles_of(len, a.max_blocks);
     if (SPLIT && cur >= base + (long long)nt * pairs) {
       base += (long long)nt * pairs;
       if (++b >= a.B) return;  // (a later request has the tiles that are left)
@@ -659,6 +662,10 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
     const int t1 = SPLIT ? (int)min((long long)nt, t0 + (end - cur)) : nt;
     const int hk = pair / RB, r0 = pair % RB * 16;
     const size_t row0 = ((size_t)b * a.H_q + (size_t)hk * G) * a.Q + r0;
+
+    // a tile's block is asked for a tile ahead, the first one's before the queries
+    const int* table = a.tables + (size_t)b * a.max_blocks;
+    int next = t0 + wave < t1 ? table[t0 + wave] : -1;
 
     // queries: dims 64 (s / 2) + 16 g + 8 (s % 2) .. + 7 for step s
     bf16x8_t qf[4][kQT];
@@ -683,7 +690,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
     float m = -INFINITY, l = 0.f;
 
     for (int t = t0 + wave; t < t1; t += 4) {
-      const int blk = a.tables[(size_t)b * a.max_blocks + t];
+      const int blk = next;
+      next = t + 4 < t1 ? table[t + 4] : -1;
       if (blk < 0 || blk >= a.n_blocks) continue;
       const size_t at = ((size_t)blk * a.H_kv + hk) * kBlockBytes;
       const float2 sc = *reinterpret_cast<const float2*>(a.scales + ((size_t)blk * a.H_kv + hk) * 2);
