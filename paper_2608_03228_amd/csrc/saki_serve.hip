@@ -110,7 +110,7 @@ __device__ __forceinline__ void sin_cos_turns(double turns, float* s, float* c) 
 // and cosines are formed once per wave.  Each lane reads both halves of its
 // pairs before it writes them: the outputs may be the inputs.  HBM bound: 16,384
 // float32 tokens of 28 + 4 heads in 100 us, 5.4 TB/s; 64 bf16 tokens of 32 + 8
-// heads, a few loads deep, in 3.6.
+// heads, a few loads deep, in 4.0.
 constexpr int kRopeWaves = 4;
 constexpr int kRopeAhead = 4;  // heads a lane has in flight
 template <typename T>
@@ -595,10 +595,10 @@ __device__ __forceinline__ Share share_of(long long total, int groups) {
 // The codes are exact in bf16; queries (float32: three terms) and weights (two
 // terms, three for float32 output) are split so that nothing but the output is
 // rounded to bf16.  HBM bound, 16 KB a tile: 8 requests of up to 131,072 keys in
-// 4 heads in 110 us, 5.35 TB/s of 590 MB fetched.  A request of 4,001 keys in 8
-// heads takes 9.9 us, and the join 4.1: a chain of reads (lengths, table, codes)
+// 4 heads in 108 us, 5.5 TB/s of 590 MB fetched.  A request of 4,001 keys in 8
+// heads takes 10.2 us, and the join 4.4: a chain of reads (lengths, table, codes)
 // with a tile a wave behind it.  Holding the next tile's codes in registers
-// (241 of them) did not shorten either, 14.2 us against 13.5 for the step.
+// (241 of them) did not shorten either, 14.2 us against 13.4 for the step.
 //
 // Without SPLIT a work-group takes one whole pair: no share to find, no
 // workspace and no join (see whole_better).
@@ -1057,11 +1057,12 @@ int saki_rope(const void* q, const void* k, int dtype, int T, int H_q, int H_kv,
   if (H_q && (!rows_ok(q, ld_q, H_q, dtype) || !rows_ok(q_out, ld_q_out, H_q, dtype))) return SAKI_ERR_ARG;
   if (H_kv && (!rows_ok(k, ld_k, H_kv, dtype) || !rows_ok(k_out, ld_k_out, H_kv, dtype))) return SAKI_ERR_ARG;
   Turns turns;
-  // powers of theta^(-2/d) by products of 64-bit significands: each within half
-  // a unit of float64's last place and 2^-56
-  const long double r = std::pow((long double)rope_theta, -2.0L / d);
-  long double f = 0.15915494309189533576888L;
-  for (int m = 0; m < d / 2; ++m, f *= r) turns.f[m] = (double)f;
+  // powers by products, within 2^-51 (3.5e-16 at theta = 500,000; 64 or 16 calls
+  // of pow are 0.3 us and more of a call of 5)
+  const double r = std::pow((double)rope_theta, -2.0 / d), r8 = std::pow((double)rope_theta, -16.0 / d);
+  double lo[8] = {1.0}, hi[8] = {0.15915494309189533577};
+  for (int i = 1; i < 8; ++i) lo[i] = lo[i - 1] * r, hi[i] = hi[i - 1] * r8;
+  for (int m = 0; m < d / 2; ++m) turns.f[m] = hi[m / 8] * lo[m % 8];
   // heads that a wave visits at once; a token's heads are split over up to that
   // many waves while there are few tokens
   const int at_once = dtype == SAKI_F32 ? 4 : 8;
