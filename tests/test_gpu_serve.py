@@ -76,6 +76,20 @@ def test_rope(T, H_q, H_kv, sections, inverse, dt):
         assert np.all(np.abs(host(y) - want) <= bound), np.max(np.abs(host(y) - want) / bound)
 
 
+def test_rope_far_and_negative_positions():
+    """Angles up to 2^31: the frequencies (within 2^-51) and the oracle's float64
+    product (2^-52) leave 1.5 * 2^-51 of the angle besides the bound of near ones."""
+    rng = np.random.default_rng(5)
+    pos = np.array([[2147483647, -2147483648, 2000000011, -1, -70001, 1 << 30]])
+    x = rounded(rng.standard_normal((6, 2, 128)), "f32")
+    got = host(S.saki_rope(dev(x), None, ints(pos))[0])
+    want = O.rope_axes(x, pos, (64,))
+    size = np.abs(x[..., :64]) + np.abs(x[..., 64:])
+    angle = np.abs(pos[0])[:, None, None] * O.ROPE_THETA ** (-np.arange(64) / 64)
+    bound = (4.5 * U + 1.5 * 2.0 ** -51 * angle) * size
+    assert np.all(np.abs(got - want) <= np.concatenate([bound, bound], -1))
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_rope_in_place_in_a_fused_projection_and_back(dt):
     """q, k slices of one [T, (H_q + 2 H_kv) d] projection, rotated in place and
