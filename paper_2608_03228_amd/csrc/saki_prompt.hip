@@ -337,7 +337,8 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
     vt = fmaxf(vt, fabsf(v[j]));
   }
 #pragma unroll
-  for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(&vals[row][c + j]) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  for (int j = 0; j < 16; j += 4)
+    *reinterpret_cast<float4*>(&vals[row][c + j]) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 #pragma unroll
   for (int m = 1; m < kWave; m <<= 1) {
     kt = fmaxf(kt, __shfl_xor(kt, m));
@@ -346,7 +347,8 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
   if (tid % kWave == 0) part[0][tid / kWave] = kt, part[1][tid / kWave] = vt;
   __syncthreads();
   const int ek = unit_exponent(fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3])), 0);
-  const int ev = unit_exponent(fmaxf(fmaxf(part[1][0], part[1][1]), fmaxf(part[1][2], part[1][3])), 200);  // zeros scale nothing down
+  // (values of zero scale no others down)
+  const int ev = unit_exponent(fmaxf(fmaxf(part[1][0], part[1][1]), fmaxf(part[1][2], part[1][3])), 200);
   const size_t id = (size_t)tile * a.H_kv + hk;
   if (tid == 0) exps[id] = make_int2(ek, ev);
   uint8_t* out = ws + id * kSplitTile;
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
     __builtin_memcpy(out + kPart + to, &lo, 16);
   }
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {  // step x = u, dim block d: lane 32 h + (dim % 32) holds keys 16 x + 4 h + {0..3, 8..11}
+  for (int u = 0; u < 2; ++u) {  // step u, dim block d: lane 32 h + (dim % 32) holds keys 16 u + 4 h + {0..3, 8..11}
     const int d = tid / 64, lane = tid % 64, h = lane / 32;
     float y[8];
 #pragma unroll
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
 // As prompt_attend_kernel, on tiles of 32 keys in parts; with KS = 2 a step
 // stages two tiles and each half of the waves takes one.
 template <int KS>
-__global__ __launch_bounds__(256, 2) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
+__global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
                                                                    const int2* __restrict__ exps) {
   __shared__ alignas(1024) uint8_t lds_a[KS * kSplitTile], lds_b[KS * kSplitTile];
   constexpr int kPart = kSplitTile / 4, kBlockRows = kRows / KS;

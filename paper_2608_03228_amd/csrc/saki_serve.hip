@@ -822,7 +822,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
           store_elems<float, kDims>((float*)out + to, y);
         else
           store_elems<__bf16, kDims>((__bf16*)out + to, y);
-      } else if constexpr (SPLIT) {  // a share has two such stretches at most: one that began before it, one that ends after it
+      } else if constexpr (SPLIT) {
+        // a share has two such stretches at most: one that began before it, one that ends after it
         float* p = ws + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartFloats;
         store_elems<float, kDims>(p + row * kHeadDim + d0, y);
         if (d0 == 0) p[kPartRows * kHeadDim + row] = M, p[kPartRows * kHeadDim + kPartRows + row] = L;

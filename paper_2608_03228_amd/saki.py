@@ -418,7 +418,6 @@ def saki_attend(values, q, top_idx, N_valid: int, keys=None, index=None, sketch:
 # ------------------------------------------------------- serving around the index
 
 CACHE_BLOCK = 64    # tokens per cache block
-CACHE_MAX_Q = 16    # queries per request and head in saki_cache_attend
 NO_WORKSPACE = 256  # a workspace size up to this: the call needs none
 
 # These calls run 4 to 10 us on the GPU for a decode step, less than a dozen
@@ -440,8 +439,8 @@ def _args():
         try:
             from . import _saki_args
         except ImportError as e:
-            raise RuntimeError("paper_2608_03228_amd/_saki_args is missing or does not load "
-                               f"({e}); build it with `python -m paper_2608_03228_amd.build`") from e
+            raise RuntimeError(f"paper_2608_03228_amd/_saki_args is missing or does not load ({e}); "
+                               "build it with `python -m paper_2608_03228_amd.build`") from e
         torch = _torch()
         _codes.update({torch.float32: F32, torch.bfloat16: BF16})
         _saki_args.refusal(_refuse)
@@ -564,9 +563,9 @@ def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse:
         ko, ldko = (kp, ldk) if k_out is k else _rows(k_out, dt, kshape, dev, "k_out")
     else:
         k_out = None
-    st = _args_mod.saki_rope(qp, kp, code, T, H_q, H_kv, d, ldq, ldk, pp, axes, sec.address, rope_theta,
-                         1 if inverse else 0, qo, ko, ldqo, ldko,
-                         cur if stream is None else stream.cuda_stream)
+    st = _args_mod.saki_rope(qp, kp, code, T, H_q, H_kv, d, ldq, ldk, pp, axes, sec.address,
+                             rope_theta, 1 if inverse else 0, qo, ko, ldqo, ldko,
+                             cur if stream is None else stream.cuda_stream)
     if st:
         _check("saki_rope", st)
     return q_out, k_out
@@ -616,8 +615,8 @@ def saki_cache_write(k, v, slots, k_cache, v_cache, scales, stream=None):
     kp, ldk = _rows(k, dt, shape, dev, "k")
     vp_, ldv = _rows(v, dt, shape, dev, "v")
     st = _args_mod.saki_cache_write(kp, vp_, code, T, H_kv, d, ldk, ldv,
-                                _array(slots, torch.int32, (T,), dev, "slots"), kc, vc, sc, n_blocks,
-                                cur if stream is None else stream.cuda_stream)
+                                    _array(slots, torch.int32, (T,), dev, "slots"), kc, vc, sc,
+                                    n_blocks, cur if stream is None else stream.cuda_stream)
     if st:
         _check("saki_cache_write", st)
     return k_cache, v_cache, scales
@@ -660,8 +659,9 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
         if ws is not None:
             wn = ws.numel()
             wp = _array(ws, torch.uint8, (wn,), dev, "ws")
-    st = _args_mod.saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp, max_blocks,
-                                 lp, ip, k, op, wp, wn, cur if stream is None else stream.cuda_stream)
+    st = _args_mod.saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp,
+                                     max_blocks, lp, ip, k, op, wp, wn,
+                                     cur if stream is None else stream.cuda_stream)
     if st:
         _check("saki_cache_attend", st)
     return out
@@ -697,8 +697,8 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
         wn = ws.numel()
         wp = _array(ws, torch.uint8, (wn,), dev, "ws")
     st = _args_mod.saki_attend_prompt(qp, kp, vp_, code, T, n - 1, H_q, H_kv, d, ldq, ldk, ldv, cp,
-                                  _array(out, dt, shape, dev, "out"), wp, wn,
-                                  cur if stream is None else stream.cuda_stream)
+                                      _array(out, dt, shape, dev, "out"), wp, wn,
+                                      cur if stream is None else stream.cuda_stream)
     if st:
         _check("saki_attend_prompt", st)
     return out
