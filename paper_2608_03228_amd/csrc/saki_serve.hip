@@ -1161,7 +1161,7 @@ size_t saki_cache_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int ma
       k > saki::kMaxK)
     return 0;
   const long long row_blocks = ((long long)(H_q / H_kv) * Q + 15) / 16;
-  if (k > 0 || Q == 0 || whole_better(B * H_kv * row_blocks, max_blocks)) return 256;
+  if (k > 0 || Q == 0 || whole_better((long long)B * H_kv * row_blocks, max_blocks)) return 256;
   const double tiles = (double)B * H_kv * row_blocks * max_blocks;
   const int groups = attend_groups(tiles > 1e9 ? 1000000000LL : (long long)tiles);
   return (size_t)groups * 2 * kPartFloats * sizeof(float);
@@ -1193,7 +1193,7 @@ int saki_cache_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q,
       hipLaunchKernelGGL((cache_lists_kernel<false>), grid, dim3(64), 0, s, a, q, top_idx, k, out);
     return launched() ? SAKI_OK : SAKI_ERR_HIP;
   }
-  const long long pairs = B * H_kv * row_blocks;
+  const long long pairs = (long long)B * H_kv * row_blocks;
   if (whole_better(pairs, max_blocks)) {
     const dim3 grid((unsigned)pairs);
     if (dtype == SAKI_F32)

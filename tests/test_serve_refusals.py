@@ -103,6 +103,11 @@ def test_cache_attend_workspace():
     assert f(1, 4, 1, 1, 1, 65) == 0
 
 
+def test_cache_attend_workspace_of_more_pairs_than_an_int_holds():
+    f = S.saki_cache_attend_workspace_bytes
+    assert f(1 << 20, 4096, 4096, 1, 20) == f(1 << 19, 4096, 4096, 1, 20) == f(1 << 19, 4, 4, 1, 20) == 256
+
+
 PROMPT = "q k v dtype T B H_q H_kv d ld_q ld_k ld_v cu out ws ws_bytes stream".split()
 
 
