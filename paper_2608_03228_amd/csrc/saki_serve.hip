@@ -903,7 +903,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups
       L += s_l[w][r] * e;
       sum += s_y[w][r][d] * e;
     }
-    sum = L > 0.f ? sum / L : 0.f;
+    sum = L == 0.f ? 0.f : sum / L;  // (a NaN stays one)
     const size_t to = (((size_t)b * a.H_q + (size_t)hk * G) * a.Q + r0 + r) * kHeadDim + part16 * 16 + d;
     if constexpr (F32)
       ((float*)out)[to] = sum;

@@ -350,6 +350,25 @@ def test_cache_attend_peaked_rows(top_idx):
     check_attend((q, codes, scales, c, tab), lens, "f32", top_idx=idx)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,top_idx", [(None, False), (70, False), (None, True)])
+def test_cache_attend_query_of_nan_stays_one(rows, top_idx, dt):
+    """A row whose query is NaN is NaN whichever way the work is divided, and the
+    other rows are what they are without it."""
+    lens = [700, 0, 3]
+    q, _, _, (k, v, s), tab = attend_case(lens, 4, 2, 2, dt, rows)
+    idx = ints(np.tile(np.arange(3), (3, 4, 2, 1))) if top_idx else None
+    clean = S.saki_cache_attend(dev(q, DT[dt]), k, v, s, ints(tab), ints(lens), top_idx=idx)
+    bad = np.zeros(q.shape[:3], bool)
+    bad[0, 1, 0] = bad[0, 3, 1] = bad[1, 2, 0] = bad[2, 0, 1] = True
+    q[bad] = np.nan
+    out = host(S.saki_cache_attend(dev(q, DT[dt]), k, v, s, ints(tab), ints(lens), top_idx=idx))
+    np.testing.assert_array_equal(out[~bad], host(clean)[~bad])
+    assert np.all(out[1] == 0)  # no key
+    bad[1] = False
+    assert np.all(np.isnan(out[bad]))
+
+
 def test_cache_attend_is_the_same_every_time_and_on_another_stream():
     lens = [3000, 10, 700, 2500]
     q, codes, scales, (k, v, s), tab = attend_case(lens, 28, 4, 1, "bf16")
