@@ -99,7 +99,7 @@ typedef __attribute__((address_space(1))) const void global_void;
 // come first in the launch.
 // KS = 2: 64 rows, and two waves share a row's keys, 32 of each tile; their
 // sums meet at the end (see halves_better).
-// Bound by power and the MFMA: 0.99-1.06 PFLOP/s at 8,192 tokens of 32 / 8
+// Bound by power and the MFMA: 0.95-1.06 PFLOP/s at 8,192 tokens of 32 / 8
 // heads depending on the card (a large bf16 matrix product reaches 1.15), the
 // MFMA 55% busy at a clock of 1.8 GHz.  Raising the waves' priority around the
 // products or the softmax changed nothing.
