@@ -506,12 +506,18 @@ def _cache_arrays(k_cache, v_cache, scales, dev):
 
 
 def _new(stream, shape, dtype, dev):
-    """A tensor that the call writes or works in: allocated on the current
-    stream, marked as used on `stream`."""
+    """A tensor that the call writes or works in, of the memory of the stream
+    that does: what the current stream's pool hands out may still be in use by
+    what is queued there, which a call on another stream does not wait for.
+    Marked as used on the current stream too, whose work reads it next."""
     torch = _torch()
-    t = torch.empty(shape, dtype=dtype, device=dev)
-    if stream is not None:
-        t.record_stream(stream)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    here = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    if here != stream:
+        t.record_stream(here)
     return t
 
 
