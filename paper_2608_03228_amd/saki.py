@@ -237,6 +237,22 @@ def _stream(stream):
     return _torch().cuda.current_stream().cuda_stream
 
 
+def _new(stream, shape, dtype, dev):
+    """A tensor that the call writes or works in, of the memory of the stream
+    that does: what the current stream's pool hands out may still be in use by
+    what is queued there, which a call on another stream does not wait for.
+    Marked as used on the current stream too, whose work reads it next."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    here = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    if here != stream:
+        t.record_stream(here)
+    return t
+
+
 def _key_dtype(keys):
     torch = _torch()
     return BF16 if keys.dtype == torch.bfloat16 else F32
@@ -253,11 +269,11 @@ def saki_calibration_moments(q_cal, k_cal, Sigma_q=None, Sigma_k=None, key_mean=
     H_kv = k_cal.shape[0]
     dev = q_cal.device
     if Sigma_q is None:
-        Sigma_q = torch.empty((H_q, d, d), dtype=torch.float64, device=dev)
+        Sigma_q = _new(stream, (H_q, d, d), torch.float64, dev)
     if Sigma_k is None:
-        Sigma_k = torch.empty((H_kv, d, d), dtype=torch.float64, device=dev)
+        Sigma_k = _new(stream, (H_kv, d, d), torch.float64, dev)
     if key_mean is None:
-        key_mean = torch.empty((H_kv, d), dtype=torch.float64, device=dev)
+        key_mean = _new(stream, (H_kv, d), torch.float64, dev)
     st = lib().saki_calibration_moments(
         qp, kp, H_q, H_kv, T, d, _dev(Sigma_q, (torch.float64,), "Sigma_q"),
         _dev(Sigma_k, (torch.float64,), "Sigma_k"), _dev(key_mean, (torch.float64,), "key_mean"),
@@ -277,7 +293,7 @@ def saki_build_index(keys, B_k, mu, r: int, sketch: str, H_q: int, index=None,
     if index is None or not _plain(H_q, r):
         nbytes = saki_index_bytes(B, H_q, N_cap, r, sketch)
     if index is None:
-        index = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=keys.device)
+        index = _new(stream, max(nbytes, 1), torch.uint8, keys.device)
     n_count = N_cap - n_begin if n_count is None else n_count
     st = lib().saki_build_index(
         kp, _key_dtype(keys), B, int(H_q), H_kv, N_cap, d, int(r),
@@ -290,7 +306,7 @@ def saki_build_index(keys, B_k, mu, r: int, sketch: str, H_q: int, index=None,
 
 def saki_index_export(index, sketch: str, B: int, H_q: int, N_cap: int, r: int, stream=None):
     torch = _torch()
-    out = torch.empty((B, H_q, N_cap, r), dtype=torch.float32, device=index.device)
+    out = _new(stream, (B, H_q, N_cap, r), torch.float32, index.device)
     st = lib().saki_index_export(_dev(index, (torch.uint8,), "index"), _DTYPES[sketch], B, H_q,
                                  N_cap, r, out.data_ptr(), _stream(stream))
     _check("saki_index_export", st)
@@ -311,11 +327,11 @@ def saki_score_topk(index, sketch: str, q, B_q, mu, H_kv: int, N_cap: int, N_val
     if ws is None or not _plain(N_valid, r, k):
         need = saki_score_topk_workspace_bytes(B, H_q, Q, N_valid, r, k, sketch, ih)
     if ws is None:
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        ws = _new(stream, max(need, 1), torch.uint8, q.device)
     if top_idx is None:
-        top_idx = torch.empty((B, H_q, Q, k), dtype=torch.int32, device=q.device)
+        top_idx = _new(stream, (B, H_q, Q, k), torch.int32, q.device)
     if with_scores and top_score is None:
-        top_score = torch.empty((B, H_q, Q, k), dtype=torch.float32, device=q.device)
+        top_score = _new(stream, (B, H_q, Q, k), torch.float32, q.device)
     pos = _dev(q_pos, (torch.int32,), "q_pos") if q_pos is not None else None
     st = lib().saki_score_topk(
         _dev(index, (torch.uint8,), "index"), _DTYPES[sketch], B, H_q, int(H_kv), ih, int(N_cap),
@@ -364,11 +380,11 @@ def saki_recall(keys, q, approx_idx, N_valid: int, q_pos=None, k: int = 64, ws=N
     if ws is None or not _plain(N_valid, k):
         need = saki_recall_workspace_bytes(B, H_q, H_kv, Q, N_valid, d, k)
     if ws is None:
-        ws = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        ws = _new(stream, max(need, 1), torch.uint8, q.device)
     if hits is None:
-        hits = torch.empty((B, H_q, Q), dtype=torch.int32, device=q.device)
+        hits = _new(stream, (B, H_q, Q), torch.int32, q.device)
     if want_exact and exact_idx is None:
-        exact_idx = torch.empty((B, H_q, Q, k), dtype=torch.int32, device=q.device)
+        exact_idx = _new(stream, (B, H_q, Q, k), torch.int32, q.device)
     pos = _dev(q_pos, (torch.int32,), "q_pos") if q_pos is not None else None
     st = lib().saki_recall(
         kp, _key_dtype(keys), qp, pos, B, H_q, H_kv, N_cap, int(N_valid), Q, d, int(k),
@@ -398,7 +414,7 @@ def saki_attend(values, q, top_idx, N_valid: int, keys=None, index=None, sketch:
     _, H_q, Q, _ = q.shape
     k = top_idx.shape[-1]
     if out is None:
-        out = torch.empty((B, H_q, Q, d), dtype=torch.float32, device=q.device)
+        out = _new(stream, (B, H_q, Q, d), torch.float32, q.device)
     recon = keys is None
     pos = _dev(q_pos, (torch.int32,), "q_pos") if q_pos is not None else None
     st = lib().saki_attend(
@@ -503,22 +519,6 @@ def _cache_arrays(k_cache, v_cache, scales, dev):
     f8 = torch.float8_e4m3fn
     return (_array(k_cache, f8, shape, dev, "k_cache"), _array(v_cache, f8, shape, dev, "v_cache"),
             _array(scales, torch.float32, (n_blocks, H_kv, 2), dev, "scales"), n_blocks, H_kv, d)
-
-
-def _new(stream, shape, dtype, dev):
-    """A tensor that the call writes or works in, of the memory of the stream
-    that does: what the current stream's pool hands out may still be in use by
-    what is queued there, which a call on another stream does not wait for.
-    Marked as used on the current stream too, whose work reads it next."""
-    torch = _torch()
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    here = torch.cuda.current_stream(dev)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=dev)
-    if here != stream:
-        t.record_stream(here)
-    return t
 
 
 _section_arrays = {}

@@ -61,3 +61,32 @@ SERVING = {
 def test_serving_calls(name, made):
     f, args, kw, n = SERVING[name]()
     check_pools(made, lambda stream: f(*args, **kw, stream=stream), n)
+
+
+def index_of(keys, B_k, mu):
+    return S.saki_build_index(keys, B_k, mu, 16, "bf16", 4)
+
+
+def index_arrays():
+    """keys, factors and mean of one sequence, 4 / 2 heads, 200 keys, r = 16."""
+    g = torch.Generator(DEV).manual_seed(1)
+    keys, B_k, mu, q = (torch.randn(s, generator=g, device=DEV)
+                        for s in ((1, 2, 200, 128), (4, 128, 16), (2, 128), (1, 4, 1, 128)))
+    return keys, B_k, mu, q, torch.zeros(1, 4, 1, 8, device=DEV, **i32)
+
+
+INDEX = {
+    "moments": lambda k, b, mu, q, li: (S.saki_calibration_moments, (zeros(4, 64, 128), zeros(2, 64, 128)), {}, 3),
+    "build": lambda k, b, mu, q, li: (S.saki_build_index, (k, b, mu, 16, "bf16", 4), {}, 1),
+    "export": lambda k, b, mu, q, li: (S.saki_index_export, (index_of(k, b, mu), "bf16", 1, 4, 200, 16), {}, 1),
+    "score": lambda k, b, mu, q, li: (S.saki_score_topk, (index_of(k, b, mu), "bf16", q, b, mu, 2, 200, 200, 16),
+                                      dict(k=8), 3),
+    "recall": lambda k, b, mu, q, li: (S.saki_recall, (k, q, li, 200), dict(k=8), 3),
+    "attend": lambda k, b, mu, q, li: (S.saki_attend, (k, q, li, 200), dict(keys=k), 1),
+}
+
+
+@pytest.mark.parametrize("name", INDEX)
+def test_index_calls(name, made):
+    f, args, kw, n = INDEX[name](*index_arrays())
+    check_pools(made, lambda stream: f(*args, **kw, stream=stream), n)
