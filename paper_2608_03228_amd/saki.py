@@ -636,7 +636,7 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
                       stream=None):
     """q [B, H_q, Q, d] (float32 or bfloat16), the cache of saki_cache_write,
     tables [B, max_blocks] and lens [B] int32, top_idx [B, H_q, Q, k] int32 (the
-    listed keys only) or None (every key).  Returns out, as q."""
+    listed keys only; none with k = 0) or None (every key).  Returns out, as q."""
     shape, dt, code = _of_floats(q, 4, "q")
     torch, dev, cur = _current()
     B, H_q, Q, d = shape
@@ -657,6 +657,11 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
     if top_idx is not None:
         k = top_idx.shape[-1]
         ip = _array(top_idx, torch.int32, (B, H_q, Q, k), dev, "top_idx")
+        if k == 0:  # lists of nothing: as lists of one entry that names no key
+            top_idx = _new(stream, (B, H_q, Q, 1), torch.int32, q.device)
+            with torch.cuda.stream(stream):
+                top_idx.fill_(-1)
+            k, ip = 1, top_idx.data_ptr()
     else:
         if ws is None:
             need = _args_mod.saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, 0)

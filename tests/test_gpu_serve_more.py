@@ -1,0 +1,31 @@
+"""Serving calls at the ends of what they take."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_serve import DT, attend_case, dev, host, ints
+
+torch = pytest.importorskip("torch")
+S = pytest.importorskip("paper_2608_03228_amd.saki")
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [None, 70])
+def test_cache_attend_lists_of_nothing(rows, dt):
+    """Lists of no entry leave every row without a key: zeros, on any stream."""
+    lens = [300, 0, 5]
+    q, _, _, (k, v, s), tab = attend_case(lens, 4, 2, 2, dt, rows)
+    args = (dev(q, DT[dt]), k, v, s, ints(tab), ints(lens))
+    idx = torch.empty(3, 4, 2, 0, dtype=torch.int32, device=DEV)
+    assert np.all(host(S.saki_cache_attend(*args, top_idx=idx)) == 0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    out = torch.full_like(args[0], 7.0)
+    side.wait_stream(torch.cuda.current_stream())
+    S.saki_cache_attend(*args, top_idx=idx, out=out, stream=side)
+    side.synchronize()
+    assert np.all(host(out) == 0)
+    with pytest.raises(ValueError):
+        S.saki_cache_attend(*args, top_idx=idx[:2])
