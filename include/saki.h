@@ -378,7 +378,7 @@ enum {
  *   pos       device int [axes, T];  sections  host int [axes], sum d/2
  *   q_out, k_out  rows ld_q_out, ld_k_out apart; each may be its input (with
  *             its ld), and overlaps no other array otherwise
- * T <= 2^26.
+ * T <= 2^26 - 4.
  */
 int saki_rope(const void* q, const void* k, int dtype, int T, int H_q, int H_kv, int d,
               size_t ld_q, size_t ld_k, const int* pos, int axes, const int* sections,

@@ -1018,7 +1018,8 @@ bool overlap(const void* p, size_t n, const void* q, size_t m) {
 }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-constexpr int kMaxTokens = 1 << 26;  // a launch's threads fit 32 bits
+constexpr int kMaxTokens = 1 << 26;
+constexpr int kMaxRopeTokens = kMaxTokens - kRopeWaves;  // 256 threads for kRopeWaves tokens: fewer than 2^32
 
 bool launched() { return hipGetLastError() == hipSuccess; }
 
@@ -1046,7 +1047,8 @@ int saki_rope(const void* q, const void* k, int dtype, int T, int H_q, int H_kv,
   if (T < 0 || H_q < 0 || H_kv < 0 || H_q > 65535 || H_kv > 65535 || d <= 0 || !(rope_theta > 0.f) ||
       !std::isfinite(rope_theta) || !sections)
     return SAKI_ERR_ARG;
-  if (d != kHeadDim || !type_ok(dtype) || axes < 1 || axes > 3 || T > kMaxTokens) return SAKI_ERR_UNSUPPORTED;
+  if (d != kHeadDim || !type_ok(dtype) || axes < 1 || axes > 3 || T > kMaxRopeTokens)
+    return SAKI_ERR_UNSUPPORTED;
   int s[3] = {0, 0, 0}, sum = 0;
   for (int i = 0; i < axes; ++i) {
     if (sections[i] < 0 || sections[i] > d / 2) return SAKI_ERR_ARG;

@@ -29,3 +29,18 @@ def test_cache_attend_lists_of_nothing(rows, dt):
     assert np.all(host(out) == 0)
     with pytest.raises(ValueError):
         S.saki_cache_attend(*args, top_idx=idx[:2])
+
+
+def test_rope_of_the_most_tokens():
+    """2^26 - 4 tokens of one bf16 head (16 GiB), in place: sampled ones as in a
+    call of their own."""
+    T = (1 << 26) - 4
+    x = torch.zeros(T, 1, 128, dtype=torch.bfloat16, device=DEV)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    at = torch.tensor([0, 1, 12345678, T // 2, T - 2, T - 1], device=DEV)
+    y = torch.randn(6, 1, 128, generator=torch.Generator(DEV).manual_seed(3), device=DEV).bfloat16()
+    x[at] = y
+    S.saki_rope(x, None, pos, q_out=x)
+    assert torch.equal(x[at], S.saki_rope(y, None, pos[at])[0])
+    x[at] = 0
+    assert not x.any()

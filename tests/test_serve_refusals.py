@@ -167,3 +167,13 @@ def test_argument_module_checks_counts_and_ranges():
             f(None, torch.float32, (2, 3), 0, "x")
         with pytest.raises(TypeError):
             f(x, torch.float32)
+
+
+def test_rope_takes_the_tokens_that_a_launch_holds(lib):
+    """A work-group of 256 takes four tokens, and a launch has fewer than 2^32
+    threads: 2^26 - 4 tokens pass (the next check refuses them), one more do not."""
+    good = [P, P, 1, 5, 4, 2, 128, 512, 256, None, 3, (C.c_int * 3)(16, 24, 24), 1e4, 0, P, P, 512, 256, None]
+    most = (1 << 26) - 4
+    assert (most + 3) // 4 * 256 < 1 << 32 <= (most + 4) // 4 * 256
+    assert change(lib.saki_rope, good, ROPE, T=most) == ARG
+    assert change(lib.saki_rope, good, ROPE, T=most + 1) == UNSUP
