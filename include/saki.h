@@ -471,9 +471,10 @@ size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv);
  *   out_t = sum_{u <= t} p_u value_u,  p = softmax(q_t . key_u / sqrt(d)),
  * every query head over the keys of its group.  Sums and softmax are float32.
  * bf16 inputs meet in exact products, and the weights are rounded to bf16 for
- * theirs.  float32 elements and weights are taken as two fp16 parts with a
- * common power of two for 32 tokens (or one query): 22 bits of each, products
- * to 2^-21.
+ * theirs.  float32 elements and weights are taken as two fp16 parts, products
+ * to 2^-21: an element to 2^-22 of itself or 2^-35 of the largest of its token
+ * and head (a query's: 2^-39), a weight to 2^-22 of itself or 2^-31 of the row's
+ * largest p_u max |value_u|, whichever is more.
  *
  *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v
  *           apart (ld up to 2^22)

@@ -9,6 +9,7 @@
 #include <climits>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "saki.h"
 #include "saki_internal.h"
@@ -281,12 +282,29 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
 // 2^e - hi), where 2^e brings the largest element of a tile (of a query's row)
 // to [2^14, 2^15).  What hi and lo leave is below 2^-22 |x|, or 2^-39 of that
 // largest element, and a product is hi hi + lo hi + hi lo, all sums in float32:
-// three fp16 products in place of one at an eighth of their rate.  4,096 tokens
-// of 28 / 4 heads: 10.7 us for the split and 350-390 for the attention (310-340
-// TFLOP/s, the MFMA 63% busy); on the float32 MFMA it took 1,237 us.
+// three fp16 products in place of one at an eighth of their rate.  A tile whose
+// tokens' sizes are more than kSpread powers of two apart is `mixed`: there each
+// token goes by its own power, so that none takes bits from another (seen or not).
+// 4,096 tokens of 28 / 4 heads: 10.7 us for the split and 350-400 for the attention
+// (310-340 TFLOP/s, the MFMA 63% busy); on the float32 MFMA it took 1,237 us.
+// Mixed tiles cost a tenth more, in halved blocks a third (5,000 tokens of 2 / 1
+// heads, every tile mixed: 178 us against 138; one such tile a prompt: 140).
 
 constexpr int kSplitKeys = 32;
 constexpr int kSplitTile = 4 * kSplitKeys * kHeadDim * 2;  // bytes: keys hi, lo, values hi, lo
+constexpr int kSpread = 4;
+
+// Exponents of a tile's keys and values (the least, of its largest elements), and
+// whether the tokens have their own.
+struct TileExps {
+  int k, v, mixed, pad;
+};
+struct SplitWorkspace {
+  uint8_t* parts;  // [tile][kSplitTile]
+  TileExps* exps;  // [tile]
+  int* own;        // [tile][key]: its exponents, the key's below, the value's above
+};
+constexpr size_t kSplitBytes = kSplitTile + sizeof(TileExps) + kSplitKeys * sizeof(int);  // of a tile
 
 __device__ __forceinline__ float ldexp_f32(float x, int e) { return __builtin_amdgcn_ldexpf(x, e); }
 
@@ -294,24 +312,29 @@ __device__ __forceinline__ float ldexp_f32(float x, int e) { return __builtin_am
 __device__ __forceinline__ int unit_exponent(float top, int of_zero) {
   return top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : of_zero;
 }
+constexpr int kNoValue = 200;  // exponent of values of zero: they scale no others down
 
-// Eight floats times 2^e as hi and lo parts.
-__device__ __forceinline__ void split_f16(const float* x, int e, f16x8_t* hi, f16x8_t* lo) {
+// Eight floats times 2^e (2^e[j]) as hi and lo parts.
+__device__ __forceinline__ void split_f16(const float* x, const int* e, f16x8_t* hi, f16x8_t* lo) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float y = ldexp_f32(x[j], e);
+    const float y = ldexp_f32(x[j], e[j]);
     (*hi)[j] = (_Float16)y;
     (*lo)[j] = (_Float16)(y - (float)(*hi)[j]);
   }
+}
+__device__ __forceinline__ void split_f16(const float* x, int e, f16x8_t* hi, f16x8_t* lo) {
+  const int all[8] = {e, e, e, e, e, e, e, e};
+  split_f16(x, all, hi, lo);
 }
 
 // Tile x of the packed prompts' keys (32 of one prompt; the tiles of prompt b
 // start at cu[b] / 32 + b): hi and lo parts of keys and values in the order in
 // which the lanes of prompt_attend_f32_kernel take them as operands, and the
 // exponents.  Reads each element once, writes as many bytes: HBM bound.
-__global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t* __restrict__ ws,
-                                                           int2* __restrict__ exps) {
-  __shared__ float part[2][4];
+__global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWorkspace ws) {
+  __shared__ int part[4][4];
+  __shared__ int own_v[kSplitKeys];
   __shared__ float vals[kSplitKeys][kHeadDim + 4];
   const int hk = blockIdx.x % a.H_kv, tile = blockIdx.x / a.H_kv;
   const Block blk = find_block(a, tile, 1, kSplitKeys);
@@ -340,18 +363,34 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
   for (int j = 0; j < 16; j += 4)
     *reinterpret_cast<float4*>(&vals[row][c + j]) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 #pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
+  for (int m = 1; m < 8; m <<= 1) {  // the row's largest
     kt = fmaxf(kt, __shfl_xor(kt, m));
     vt = fmaxf(vt, __shfl_xor(vt, m));
   }
-  if (tid % kWave == 0) part[0][tid / kWave] = kt, part[1][tid / kWave] = vt;
+  int ek = unit_exponent(kt, 0), ev = unit_exponent(vt, kNoValue);
+  // least and largest exponents: of keys that are not zero, of values
+  constexpr int kFar = 1 << 20;
+  int lim[4] = {kt > 0.f ? ek : kFar, kt > 0.f ? -ek : kFar, in ? ev : kFar, in ? -ev : kFar};
+#pragma unroll
+  for (int m = 8; m < kWave; m <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lim[i] = min(lim[i], __shfl_xor(lim[i], m));
+  if (tid % kWave == 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[i][tid / kWave] = lim[i];
   __syncthreads();
-  const int ek = unit_exponent(fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3])), 0);
-  // (values of zero scale no others down)
-  const int ev = unit_exponent(fmaxf(fmaxf(part[1][0], part[1][1]), fmaxf(part[1][2], part[1][3])), 200);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) lim[i] = min(min(part[i][0], part[i][1]), min(part[i][2], part[i][3]));
+  const bool keys = lim[0] != kFar;
+  const bool mixed = (keys && -lim[1] - lim[0] > kSpread) || -lim[3] - lim[2] > kSpread;
   const size_t id = (size_t)tile * a.H_kv + hk;
-  if (tid == 0) exps[id] = make_int2(ek, ev);
-  uint8_t* out = ws + id * kSplitTile;
+  if (!mixed) ek = keys ? lim[0] : 0, ev = lim[2];
+  if (tid % 8 == 0) {
+    own_v[row] = ev;
+    ws.own[id * kSplitKeys + row] = (ek & 0xffff) | (int)((uint32_t)ev << 16);
+  }
+  if (tid == 0) ws.exps[id] = TileExps{keys ? lim[0] : 0, lim[2], mixed, 0};
+  uint8_t* out = ws.parts + id * kSplitTile;
   constexpr int kPart = kSplitTile / 4;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {  // dims 16 x + 8 h of key `row`: step x = c / 16, lane 32 h + row
@@ -361,14 +400,20 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
     __builtin_memcpy(out + to, &hi, 16);
     __builtin_memcpy(out + kPart + to, &lo, 16);
   }
+  __syncthreads();  // own_v
 #pragma unroll
   for (int u = 0; u < 2; ++u) {  // step u, dim block d: lane 32 h + (dim % 32) holds keys 16 u + 4 h + {0..3, 8..11}
     const int d = tid / 64, lane = tid % 64, h = lane / 32;
     float y[8];
+    int e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = vals[16 * u + 4 * h + j % 4 + 8 * (j / 4)][32 * d + lane % 32];
+    for (int j = 0; j < 8; ++j) {
+      const int key = 16 * u + 4 * h + j % 4 + 8 * (j / 4);
+      y[j] = vals[key][32 * d + lane % 32];
+      e[j] = own_v[key];
+    }
     f16x8_t hi, lo;
-    split_f16(y, ev, &hi, &lo);
+    split_f16(y, e, &hi, &lo);
     const int to = (4 * u + d) * 1024 + lane * 16;
     __builtin_memcpy(out + 2 * kPart + to, &hi, 16);
     __builtin_memcpy(out + 3 * kPart + to, &lo, 16);
@@ -377,9 +422,20 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, uint8_t
 
 // As prompt_attend_kernel, on tiles of 32 keys in parts; with KS = 2 a step
 // stages two tiles and each half of the waves takes one.
+//
+// Weights are split into fp16 parts too, whose least step is 2^-24: they are
+// scaled by what a key adds to the sums, its weight times its largest value, and
+// not by the weight alone.  A row behind a sink (a key that takes the weight, its
+// value near zero) or behind unattended keys of huge values keeps its 22 bits:
+// with c the running maximum of log2(weight) less the values' exponent, a
+// weight is held as p 2^(C - e), at most 2^15, where C = 15 - kRoom - (c - m); C is
+// a whole number, so that this scaling is exact.  The step is then 2^-35 of the
+// largest of the row's p 2^-e, 2^-31 of its largest p |v| (a tile's tokens are up
+// to 2^kSpread apart).
+constexpr float kRoom = 4.f;      // powers of two that c may be passed by before the sums are moved
+constexpr int kNothing = 1000;    // C of a row without a key
 template <int KS>
-__global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptArgs a, const uint8_t* __restrict__ ws,
-                                                                   const int2* __restrict__ exps) {
+__global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptArgs a, SplitWorkspace ws) {
   __shared__ alignas(1024) uint8_t lds_a[KS * kSplitTile], lds_b[KS * kSplitTile];
   constexpr int kPart = kSplitTile / 4, kBlockRows = kRows / KS;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -389,7 +445,7 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
   const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kBlockRows);
   const int n = lane % 32, h = lane / 32;
   // this wave's 32 rows and which of a step's KS tiles it takes
-  const int rw = KS == 1 ? wave * 32 : wave % 2 * 32, b0 = KS == 1 ? 0 : wave / 2;
+  const int rw = KS == 1 ? wave * 32 : wave % 2 * 32, b0 = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave / 2);
   const int row = min(rw + n, n_rows - 1) + blk.row0;
   const int pos = row / G;
   const float* qp = (const float*)a.q + (size_t)(blk.start + pos) * a.ld_q + (size_t)(hk * G + row % G) * kHeadDim;
@@ -416,7 +472,7 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
       const int t = min(step * KS + j, n_tiles - 1);
-      const uint8_t* p = ws + (tile0 + (size_t)t * a.H_kv) * kSplitTile + wave * 8192 + lane * 16;
+      const uint8_t* p = ws.parts + (tile0 + (size_t)t * a.H_kv) * kSplitTile + wave * 8192 + lane * 16;
 #pragma unroll
       for (int u = 0; u < 8; ++u)
         __builtin_amdgcn_global_load_lds((global_void*)(p + u * 1024),
@@ -430,19 +486,18 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-  // m: the running maximum in powers of two; o and l hold sums of 2^6 p (so that
-  // fp16 holds them, 2^(6 + kSlack) at most), and o of values times 2^E, E the
-  // least exponent of the tiles so far
-  float m = -INFINITY, l = 0.f;
-  int E = INT_MAX;
-  auto tile = [&](int step, const uint8_t* kt, uint8_t* next) __attribute__((always_inline)) {
+  // m: the running maximum in powers of two, that of the weights' sum l; o holds
+  // sums of p times the values times 2^C
+  float m = -INFINITY, c = -INFINITY, l = 0.f;
+  int C = kNothing;
+  auto tile = [&](int step, const uint8_t* kt, uint8_t* next, auto mixed) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the step's tiles
     __syncthreads();
     if (step + 1 < n_steps) stage(step + 1, next);
     const int t = step * KS + b0;
     if (t * kSplitKeys > pos_hi) return;
     kt += b0 * kSplitTile;
-    const int2 ex = exps[tile0 + (size_t)t * a.H_kv];
+    const TileExps ex = ws.exps[tile0 + (size_t)t * a.H_kv];
     kt += lane * 16;
     f32x16_t s;
 #pragma unroll
@@ -456,36 +511,73 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
       s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, ql[x], s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, qh[x], s, 0, 0, 0);
     }
+    int own[16];
+    if constexpr (mixed) {
+      const int* p = ws.own + (tile0 + (size_t)t * a.H_kv) * kSplitKeys + 4 * h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) __builtin_memcpy(own + 4 * i, p + 8 * i, 16);
+    }
+    auto own_k = [&](int i) { return (int)(short)own[i]; };
+    auto own_v = [&](int i) { return own[i] >> 16; };
+    // (in range, so that neither 0 times it nor -inf times it is a NaN)
+    auto factor = [&](int e) { return fminf(fmaxf(ldexp_f32(kScale * kLog2e, -(eq + e)), 0x1p-120f), 0x1p120f); };
+    float f = 1.f;
+    if constexpr (mixed) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] *= factor(own_k(i));
+    } else {
+      f = factor(ex.k);
+    }
     if (t * kSplitKeys + kSplitKeys - 1 > pos_lo) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (t * kSplitKeys + 8 * (i / 4) + 4 * h + i % 4 > pos) s[i] = -INFINITY;
     }
-    const float f = fmaxf(ldexp_f32(kScale * kLog2e, -(eq + ex.x)), 0x1p-120f);  // (0 times -inf is none)
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = fmaxf(top, swap32(top)) * f;
-    if (__any(top > m + kSlack) || ex.y < E) {
+    // a key 2^100 below the row's largest weight is scaled no further up
+    float adds = fmaxf(mixed ? -INFINITY : top, fmaxf(m, top) - 100.f) - (float)ex.v;
+    if constexpr (mixed) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i] - (float)own_v(i));
+      adds = fmaxf(adds, fmaxf(most, swap32(most)));
+    }
+    if (__any(top > m + kSlack || adds > c + kRoom)) {
       const float m1 = fmaxf(m, top);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m1);
       m = m1;
       l *= keep;
-      const int E1 = min(E, ex.y);
-      const float turn = E == INT_MAX ? 0.f : ldexp_f32(keep, E1 - E);
-      E = E1;
+      c = fmaxf(c, adds);
+      const float apart = fminf(fmaxf(c - m, -400.f), 400.f);  // (a row of NaN or infinities: any)
+      const int C1 = m == -INFINITY ? kNothing : (int)floorf(15.f - kRoom - apart);
+      const float turn = ldexp_f32(keep, C1 - C);
+      C = C1;
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[d] *= turn;
     }
-    const float shift = KS > 1 && m == -INFINITY ? 0.f : 6.f - m, part = ldexp_f32(1.f, E - ex.y);
+    const float shift = m == -INFINITY ? 0.f : -m;
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], f, shift));
+      l += p[i];
+    }
+    if constexpr (mixed) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = ldexp_f32(p[i], C - own_v(i));
+    } else {
+      const float part = ldexp_f32(1.f, C - ex.v);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] *= part;
+    }
     f16x8_t ph[2], pl[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float p = __builtin_amdgcn_exp2f(fmaf(s[i], f, shift));
-      l += p;
-      p *= part;
-      ph[i / 8][i % 8] = (_Float16)p;
-      pl[i / 8][i % 8] = (_Float16)(p - (float)ph[i / 8][i % 8]);
+      ph[i / 8][i % 8] = (_Float16)p[i];
+      pl[i / 8][i % 8] = (_Float16)(p[i] - (float)ph[i / 8][i % 8]);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -499,17 +591,31 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph[x], o[d], 0, 0, 0);
       }
   };
+  // Mixed tiles have a loop of their own (their weights in the same loop took 2 to
+  // 15% from all, or spilled), entered by two steps whose tiles are among them
+  uint64_t mixed_tiles = 0;  // of the 64 that this step's are among
+  auto mixed_next = [&](int step) {
+    const int t = step * KS;
+    if (t % kWave == 0)
+      mixed_tiles = __ballot(ws.exps[tile0 + (size_t)min(t + lane, n_tiles - 1) * a.H_kv].mixed != 0);
+    return (mixed_tiles >> (t % kWave) & ((1u << 2 * KS) - 1)) != 0;
+  };
+  auto two_steps = [&](int step, auto mixed) __attribute__((always_inline)) {
+    tile(step, lds_a, lds_b, mixed);
+    if (step + 1 < n_steps) tile(step + 1, lds_b, lds_a, mixed);
+  };
+  bool mix = mixed_next(0);
   stage(0, lds_a);
-  for (int step = 0; step < n_steps; step += 2) {
-    tile(step, lds_a, lds_b);
-    if (step + 1 < n_steps) tile(step + 1, lds_b, lds_a);
+  for (int step = 0; step < n_steps;) {
+    for (; step < n_steps && !mix; step += 2, mix = mixed_next(step)) two_steps(step, std::false_type());
+    for (; step < n_steps && mix; step += 2, mix = mixed_next(step)) two_steps(step, std::true_type());
   }
   l += swap32(l);
   if constexpr (KS == 2) {  // the second waves' sums join the first ones', through the tiles' memory
     __syncthreads();
     float* x = (float*)(rw ? lds_b : lds_a);  // [64 sums][lane]
     __shared__ float ml[2][2][kWave];
-    __shared__ int es[2];
+    __shared__ int cs[2][kWave];
     if (b0 == 1) {
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -517,17 +623,17 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
         for (int i = 0; i < 16; ++i) x[(16 * d + i) * kWave + lane] = o[d][i];
       ml[rw / 32][0][lane] = m;
       ml[rw / 32][1][lane] = l;
-      es[rw / 32] = E;
+      cs[rw / 32][lane] = C;
     }
     __syncthreads();
     if (b0 == 1) return;
     const float m2 = ml[rw / 32][0][lane], l2 = ml[rw / 32][1][lane], m1 = fmaxf(m, m2);
-    const int E2 = es[rw / 32], E1 = min(E, E2);  // (the first waves have a tile each)
+    const int C2 = cs[rw / 32][lane], C1 = min(C, C2);  // (a row's first key is in the first waves' part)
     float e1 = __builtin_amdgcn_exp2f(m - m1), e2 = __builtin_amdgcn_exp2f(m2 - m1);
     l = l * e1 + l2 * e2;
-    e1 = ldexp_f32(e1, E1 - E);
-    e2 = E2 == INT_MAX ? 0.f : ldexp_f32(e2, E1 - E2);
-    E = E1;
+    e1 = ldexp_f32(e1, C1 - C);
+    e2 = ldexp_f32(e2, C1 - C2);
+    C = C1;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -542,7 +648,7 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
       for (int i = 0; i < 16; i += 4) {
         float y[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = ldexp_f32(o[d][i + j] * inv, -E);
+        for (int j = 0; j < 4; ++j) y[j] = ldexp_f32(o[d][i + j] * inv, -C);
         *reinterpret_cast<float4*>(out + 32 * d + 2 * i + 4 * h) = make_float4(y[0], y[1], y[2], y[3]);
       }
   }
@@ -576,8 +682,7 @@ bool halves_better(long long blocks, int T, int B) {
 
 constexpr size_t kMaxLd = 1 << 22;  // a tile's byte offsets fit 32 bits
 
-// Tiles of float32 parts that all prompts have, at most, and the workspace: the
-// exponents behind the tiles.
+// Tiles of float32 parts that all prompts have, at most.
 long long split_tiles(int T, int B) { return (long long)T / kSplitKeys + B; }
 
 }  // namespace
@@ -587,7 +692,7 @@ extern "C" {
 size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv) {
   if (T < 0 || B < 0 || H_kv <= 0 || (dtype != SAKI_F32 && dtype != SAKI_BF16)) return 0;
   if (dtype == SAKI_BF16 || T == 0 || B == 0) return 256;
-  return (size_t)split_tiles(T, B) * H_kv * (kSplitTile + sizeof(int2));
+  return (size_t)split_tiles(T, B) * H_kv * kSplitBytes;
 }
 
 int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, int T, int B, int H_q, int H_kv,
@@ -620,16 +725,16 @@ int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, i
   if (!ws || ws_bytes < saki_attend_prompt_workspace_bytes(dtype, T, B, H_kv) || reinterpret_cast<uintptr_t>(ws) % 16)
     return SAKI_ERR_WORKSPACE;
   const long long n = split_tiles(T, B) * H_kv;
-  uint8_t* parts = (uint8_t*)ws;
-  int2* exps = (int2*)(parts + (size_t)n * kSplitTile);
-  hipLaunchKernelGGL(prompt_split_kernel, dim3((unsigned)n), dim3(256), 0, s, a, parts, exps);
+  SplitWorkspace w;  // the exponents stand behind the parts
+  w.parts = (uint8_t*)ws;
+  w.exps = (TileExps*)(w.parts + (size_t)n * kSplitTile);
+  w.own = (int*)(w.exps + n);
+  hipLaunchKernelGGL(prompt_split_kernel, dim3((unsigned)n), dim3(256), 0, s, a, w);
   if (hipGetLastError() != hipSuccess) return SAKI_ERR_HIP;
   if (halves)
-    hipLaunchKernelGGL((prompt_attend_f32_kernel<2>), grid, dim3(256), 0, s, a, (const uint8_t*)parts,
-                       (const int2*)exps);
+    hipLaunchKernelGGL((prompt_attend_f32_kernel<2>), grid, dim3(256), 0, s, a, w);
   else
-    hipLaunchKernelGGL((prompt_attend_f32_kernel<1>), grid, dim3(256), 0, s, a, (const uint8_t*)parts,
-                       (const int2*)exps);
+    hipLaunchKernelGGL((prompt_attend_f32_kernel<1>), grid, dim3(256), 0, s, a, w);
   return hipGetLastError() == hipSuccess ? SAKI_OK : SAKI_ERR_HIP;
 }
 
