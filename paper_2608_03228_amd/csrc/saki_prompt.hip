@@ -294,10 +294,11 @@ constexpr int kSplitKeys = 32;
 constexpr int kSplitTile = 4 * kSplitKeys * kHeadDim * 2;  // bytes: keys hi, lo, values hi, lo
 constexpr int kSpread = 4;
 
-// Exponents of a tile's keys and values (the least, of its largest elements), and
-// whether the tokens have their own.
+// Exponents of a tile's keys and values (the least, of its largest elements),
+// whether the tokens have their own, and the tokens whose values are not all finite.
 struct TileExps {
-  int k, v, mixed, pad;
+  int k, v, mixed;
+  uint32_t odd_values;
 };
 struct SplitWorkspace {
   uint8_t* parts;  // [tile][kSplitTile]
@@ -312,7 +313,10 @@ __device__ __forceinline__ float ldexp_f32(float x, int e) { return __builtin_am
 __device__ __forceinline__ int unit_exponent(float top, int of_zero) {
   return top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : of_zero;
 }
-constexpr int kNoValue = 200;  // exponent of values of zero: they scale no others down
+constexpr int kNoValue = 200;     // exponent of values of zero: they scale no others down
+constexpr int kOddKey = -0x8000;  // that of a key whose elements are not all finite
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
 // Eight floats times 2^e (2^e[j]) as hi and lo parts.
 __device__ __forceinline__ void split_f16(const float* x, const int* e, f16x8_t* hi, f16x8_t* lo) {
@@ -331,10 +335,12 @@ __device__ __forceinline__ void split_f16(const float* x, int e, f16x8_t* hi, f1
 // Tile x of the packed prompts' keys (32 of one prompt; the tiles of prompt b
 // start at cu[b] / 32 + b): hi and lo parts of keys and values in the order in
 // which the lanes of prompt_attend_f32_kernel take them as operands, and the
-// exponents.  Reads each element once, writes as many bytes: HBM bound.
+// exponents.  Elements that are not finite are zero in the parts, as they would
+// reach the rows that do not see them (0 times a NaN is one): their tiles are mixed
+// and say where they are.  Reads each element once, writes as many bytes: HBM bound.
 __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWorkspace ws) {
   __shared__ int part[4][4];
-  __shared__ int own_v[kSplitKeys];
+  __shared__ int own_v[kSplitKeys], odd[kSplitKeys];
   __shared__ float vals[kSplitKeys][kHeadDim + 4];
   const int hk = blockIdx.x % a.H_kv, tile = blockIdx.x / a.H_kv;
   const Block blk = find_block(a, tile, 1, kSplitKeys);
@@ -347,6 +353,7 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWo
   const float* kp = (const float*)a.k + tok * a.ld_k + (size_t)hk * kHeadDim + c;
   const float* vp = (const float*)a.v + tok * a.ld_v + (size_t)hk * kHeadDim + c;
   float kt = 0.f, vt = 0.f;
+  bool odd_k = false, odd_v = false;
 #pragma unroll
   for (int j = 0; j < 16; j += 4) {
     const float4 x = *reinterpret_cast<const float4*>(kp + j), y = *reinterpret_cast<const float4*>(vp + j);
@@ -356,6 +363,10 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWo
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     if (!in) k[j] = v[j] = 0.f;
+    odd_k |= !finite(k[j]);
+    odd_v |= !finite(v[j]);
+    if (!finite(k[j])) k[j] = 0.f;
+    if (!finite(v[j])) v[j] = 0.f;
     kt = fmaxf(kt, fabsf(k[j]));
     vt = fmaxf(vt, fabsf(v[j]));
   }
@@ -366,11 +377,13 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWo
   for (int m = 1; m < 8; m <<= 1) {  // the row's largest
     kt = fmaxf(kt, __shfl_xor(kt, m));
     vt = fmaxf(vt, __shfl_xor(vt, m));
+    odd_k |= __shfl_xor((int)odd_k, m);
+    odd_v |= __shfl_xor((int)odd_v, m);
   }
   int ek = unit_exponent(kt, 0), ev = unit_exponent(vt, kNoValue);
   // least and largest exponents: of keys that are not zero, of values
   constexpr int kFar = 1 << 20;
-  int lim[4] = {kt > 0.f ? ek : kFar, kt > 0.f ? -ek : kFar, in ? ev : kFar, in ? -ev : kFar};
+  int lim[4] = {kt > 0.f ? ek : kFar, kt > 0.f ? -ek : kFar, in ? ev : kFar, odd_k || odd_v ? -kFar : in ? -ev : kFar};
 #pragma unroll
   for (int m = 8; m < kWave; m <<= 1)
 #pragma unroll
@@ -387,9 +400,9 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWo
   if (!mixed) ek = keys ? lim[0] : 0, ev = lim[2];
   if (tid % 8 == 0) {
     own_v[row] = ev;
-    ws.own[id * kSplitKeys + row] = (ek & 0xffff) | (int)((uint32_t)ev << 16);
+    odd[row] = odd_v;
+    ws.own[id * kSplitKeys + row] = ((odd_k ? kOddKey : ek) & 0xffff) | (int)((uint32_t)ev << 16);
   }
-  if (tid == 0) ws.exps[id] = TileExps{keys ? lim[0] : 0, lim[2], mixed, 0};
   uint8_t* out = ws.parts + id * kSplitTile;
   constexpr int kPart = kSplitTile / 4;
 #pragma unroll
@@ -400,7 +413,11 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWo
     __builtin_memcpy(out + to, &hi, 16);
     __builtin_memcpy(out + kPart + to, &lo, 16);
   }
-  __syncthreads();  // own_v
+  __syncthreads();  // own_v, odd
+  if (tid < kWave) {
+    const uint32_t odd_values = (uint32_t)__ballot(tid < kSplitKeys && odd[tid % kSplitKeys]);
+    if (tid == 0) ws.exps[id] = TileExps{keys ? lim[0] : 0, lim[2], mixed, odd_values};
+  }
 #pragma unroll
   for (int u = 0; u < 2; ++u) {  // step u, dim block d: lane 32 h + (dim % 32) holds keys 16 u + 4 h + {0..3, 8..11}
     const int d = tid / 64, lane = tid % 64, h = lane / 32;
@@ -418,6 +435,17 @@ __global__ __launch_bounds__(256) void prompt_split_kernel(PromptArgs a, SplitWo
     __builtin_memcpy(out + 2 * kPart + to, &hi, 16);
     __builtin_memcpy(out + 3 * kPart + to, &lo, 16);
   }
+}
+
+// Adds a value's elements that are not finite to a lane's sums.
+__device__ __forceinline__ void add_odd(const float* v, f32x16_t* o) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float x = v[32 * d + 8 * (i / 4) + i % 4];
+      if (!finite(x)) o[d][i] += x;
+    }
 }
 
 // As prompt_attend_kernel, on tiles of 32 keys in parts; with KS = 2 a step
@@ -524,7 +552,7 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
     float f = 1.f;
     if constexpr (mixed) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] *= factor(own_k(i));
+      for (int i = 0; i < 16; ++i) s[i] = own_k(i) == kOddKey ? NAN : s[i] * factor(own_k(i));
     } else {
       f = factor(ex.k);
     }
@@ -589,6 +617,11 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vl, ph[x], o[d], 0, 0, 0);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, pl[x], o[d], 0, 0, 0);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph[x], o[d], 0, 0, 0);
+      }
+    if constexpr (mixed)
+      for (uint32_t odd = ex.odd_values; odd; odd &= odd - 1) {
+        const int u = t * kSplitKeys + __builtin_ctz(odd);
+        if (u <= pos) add_odd((const float*)a.v + (size_t)(blk.start + u) * a.ld_v + hk * kHeadDim + 4 * h, o);
       }
   };
   // Mixed tiles have a loop of their own (their weights in the same loop took 2 to
