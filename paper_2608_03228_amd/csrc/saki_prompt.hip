@@ -287,8 +287,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(PromptArgs a) {
 // token goes by its own power, so that none takes bits from another (seen or not).
 // 4,096 tokens of 28 / 4 heads: 10.7 us for the split and 350-400 for the attention
 // (310-340 TFLOP/s, the MFMA 63% busy); on the float32 MFMA it took 1,237 us.
-// Mixed tiles cost a tenth more, in halved blocks a third (5,000 tokens of 2 / 1
-// heads, every tile mixed: 178 us against 138; one such tile a prompt: 140).
+// Every tile mixed: 414 us in all against 395; in halved blocks (5,000 tokens of
+// 2 / 1 heads) 199 against 137, and 139 with the first one mixed.
 
 constexpr int kSplitKeys = 32;
 constexpr int kSplitTile = 4 * kSplitKeys * kHeadDim * 2;  // bytes: keys hi, lo, values hi, lo
@@ -457,9 +457,9 @@ __device__ __forceinline__ void add_odd(const float* v, f32x16_t* o) {
 // value near zero) or behind unattended keys of huge values keeps its 22 bits:
 // with c the running maximum of log2(weight) less the values' exponent, a
 // weight is held as p 2^(C - e), at most 2^15, where C = 15 - kRoom - (c - m); C is
-// a whole number, so that this scaling is exact.  The step is then 2^-35 of the
-// largest of the row's p 2^-e, 2^-31 of its largest p |v| (a tile's tokens are up
-// to 2^kSpread apart).
+// a whole number, so that this scaling is exact.  What the parts leave of a weight
+// is then 2^-35 of the largest of the row's p 2^-e, and what that takes from the
+// sums 2^-30 of its largest p |v| (a tile's tokens are up to 2^kSpread apart).
 constexpr float kRoom = 4.f;      // powers of two that c may be passed by before the sums are moved
 constexpr int kNothing = 1000;    // C of a row without a key
 template <int KS>
@@ -621,11 +621,12 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
     if constexpr (mixed)
       for (uint32_t odd = ex.odd_values; odd; odd &= odd - 1) {
         const int u = t * kSplitKeys + __builtin_ctz(odd);
-        if (u <= pos) add_odd((const float*)a.v + (size_t)(blk.start + u) * a.ld_v + hk * kHeadDim + 4 * h, o);
+        if (__builtin_expect(u <= pos, 0)) add_odd((const float*)a.v + (size_t)(blk.start + u) * a.ld_v + hk * kHeadDim + 4 * h, o);
       }
   };
   // Mixed tiles have a loop of their own (their weights in the same loop took 2 to
-  // 15% from all, or spilled), entered by two steps whose tiles are among them
+  // 15% from all, or spilled), entered by two steps whose tiles are among them; said
+  // to be rare, so that it stands apart from the other one (5% of its time)
   uint64_t mixed_tiles = 0;  // of the 64 that this step's are among
   auto mixed_next = [&](int step) {
     const int t = step * KS;
@@ -640,8 +641,8 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
   bool mix = mixed_next(0);
   stage(0, lds_a);
   for (int step = 0; step < n_steps;) {
-    for (; step < n_steps && !mix; step += 2, mix = mixed_next(step)) two_steps(step, std::false_type());
-    for (; step < n_steps && mix; step += 2, mix = mixed_next(step)) two_steps(step, std::true_type());
+    for (; step < n_steps && __builtin_expect(!mix, 1); step += 2, mix = mixed_next(step)) two_steps(step, std::false_type());
+    for (; step < n_steps && __builtin_expect(mix, 0); step += 2, mix = mixed_next(step)) two_steps(step, std::true_type());
   }
   l += swap32(l);
   if constexpr (KS == 2) {  // the second waves' sums join the first ones', through the tiles' memory
