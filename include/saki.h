@@ -475,7 +475,8 @@ size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv);
  * to 2^-21: an element to 2^-22 of itself or 2^-35 of the largest of its token
  * and head (a query's: 2^-39), what a key adds to 2^-22 of itself or 2^-30 of the
  * row's largest p_u max |value_u|, whichever is more; a key with an element that
- * is not finite scores NaN.
+ * is not finite scores NaN.  Tokens that a row does not see leave it as it is,
+ * whatever they hold.
  *
  *   q       device [T, H_q, d] rows ld_q apart;  k, v [T, H_kv, d] rows ld_k, ld_v
  *           apart (ld up to 2^22)
