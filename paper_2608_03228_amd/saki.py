@@ -542,30 +542,35 @@ def _sections(sections, axes, d):
 
 def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse: bool = False,
               q_out=None, k_out=None, stream=None):
-    """q [T, H_q, d], k [T, H_kv, d] (or None), float32 or bfloat16; pos [T] or
-    [axes, T] int32; sections: pairs of each axis (sum d/2; one axis needs
-    none).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
-    shape, dt, code = _of_floats(q, 3, "q")
+    """q [T, H_q, d], k [T, H_kv, d] (one of them may be None), float32 or
+    bfloat16; pos [T] or [axes, T] int32; sections: pairs of each axis (sum d/2;
+    one axis needs none).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    x, name = (k, "k") if q is None else (q, "q")
+    shape, dt, code = _of_floats(x, 3, name)
     torch, dev, cur = _current()
-    T, H_q, d = shape
-    qp, ldq = _rows(q, dt, shape, dev, "q")
+    T, _, d = shape
     if pos.dim() == 1:
         axes, pp = 1, _array(pos, torch.int32, (T,), dev, "pos")
     else:
         axes = pos.shape[0]
         pp = _array(pos, torch.int32, (axes, T), dev, "pos")
     sec = _sections(sections, axes, d)
-    if q_out is None:
-        q_out = _new(stream, shape, dt, q.device)
-    qo, ldqo = (qp, ldq) if q_out is q else _rows(q_out, dt, shape, dev, "q_out")
-    H_kv = ldk = ldko = 0
-    kp = ko = None
+    H_q = ldq = ldqo = H_kv = ldk = ldko = 0
+    qp = qo = kp = ko = None
+    if q is not None:
+        H_q = shape[1]
+        qp, ldq = _rows(q, dt, shape, dev, "q")
+        if q_out is None:
+            q_out = _new(stream, shape, dt, q.device)
+        qo, ldqo = (qp, ldq) if q_out is q else _rows(q_out, dt, shape, dev, "q_out")
+    else:
+        q_out = None
     if k is not None:
         H_kv = _heads(k, "k")
         kshape = (T, H_kv, d)
         kp, ldk = _rows(k, dt, kshape, dev, "k")
         if k_out is None:
-            k_out = _new(stream, kshape, dt, q.device)
+            k_out = _new(stream, kshape, dt, k.device)
         ko, ldko = (kp, ldk) if k_out is k else _rows(k_out, dt, kshape, dev, "k_out")
     else:
         k_out = None

@@ -44,3 +44,17 @@ def test_rope_of_the_most_tokens():
     assert torch.equal(x[at], S.saki_rope(y, None, pos[at])[0])
     x[at] = 0
     assert not x.any()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rope_of_keys_alone(dt):
+    """Keys without queries, as the C entry point takes them."""
+    x = torch.randn(9, 3, 128, generator=torch.Generator(DEV).manual_seed(4), device=DEV).to(DT[dt])
+    pos = ints(range(100, 109))
+    want, _ = S.saki_rope(x, None, pos)
+    q, k = S.saki_rope(None, x, pos)
+    assert q is None and torch.equal(k, want)
+    out = torch.empty_like(x)
+    assert S.saki_rope(None, x, pos, k_out=out)[1] is out and torch.equal(out, want)
+    with pytest.raises(ValueError):
+        S.saki_rope(None, None, pos)
