@@ -465,13 +465,18 @@ def _args():
     return _args_mod
 
 
-def _current():
-    """The current device's index and its current stream."""
+def _current(stream):
+    """The current device's index and the handle of the stream to launch on, one
+    of that device's (None: its current one)."""
     torch = _torch()
-    if _raw_stream is not None and _get_device is not None:
+    if stream is None and _raw_stream is not None and _get_device is not None:
         dev = _get_device()
         return torch, dev, _raw_stream(dev)
-    return torch, torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream
+    dev = torch.cuda.current_device() if _get_device is None else _get_device()
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"stream is on cuda:{stream.device_index}, not on the current device "
+                         f"(cuda:{dev})")
+    return torch, dev, _stream(stream)
 
 
 def _refuse(t, dtype, shape, dev, name):
@@ -547,7 +552,7 @@ def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse:
     one axis needs none).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
     x, name = (k, "k") if q is None else (q, "q")
     shape, dt, code = _of_floats(x, 3, name)
-    torch, dev, cur = _current()
+    torch, dev, cur = _current(stream)
     T, _, d = shape
     if pos.dim() == 1:
         axes, pp = 1, _array(pos, torch.int32, (T,), dev, "pos")
@@ -576,7 +581,7 @@ def saki_rope(q, k, pos, sections=None, rope_theta: float = ROPE_THETA, inverse:
         k_out = None
     st = _args_mod.saki_rope(qp, kp, code, T, H_q, H_kv, d, ldq, ldk, pp, axes, sec.address,
                              rope_theta, 1 if inverse else 0, qo, ko, ldqo, ldko,
-                             cur if stream is None else stream.cuda_stream)
+                             cur)
     if st:
         _check("saki_rope", st)
     return q_out, k_out
@@ -590,7 +595,7 @@ def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=No
     _args()
     if not tables.is_cuda:
         raise ValueError("tables must be a CUDA (HIP) tensor")
-    torch, dev, cur = _current()
+    torch, dev, cur = _current(stream)
     i32 = torch.int32
     if len(tables.shape) != 2 or len(slots.shape) != 1 or len(free_blocks.shape) != 1:
         raise ValueError("tables must be [B, max_blocks], slots [T] and free_blocks [n_free]")
@@ -608,7 +613,7 @@ def saki_block_tables(ctx_lens, new_lens, free_blocks, tables, slots, pos, cu=No
         _array(tables, i32, (B, max_blocks), dev, "tables"), max_blocks,
         _array(slots, i32, (T,), dev, "slots"), _array(pos, i32, (T,), dev, "pos"), T,
         _array(cu, i32, (B + 1,), dev, "cu"), _array(lens, i32, (B,), dev, "lens"),
-        _array(counts, i32, (2,), dev, "counts"), cur if stream is None else stream.cuda_stream)
+        _array(counts, i32, (2,), dev, "counts"), cur)
     if st:
         _check("saki_block_tables", st)
     return tables, slots, pos, cu, lens, counts
@@ -619,7 +624,7 @@ def saki_cache_write(k, v, slots, k_cache, v_cache, scales, stream=None):
     v_cache [n_blocks, H_kv, 64, d] (float8_e4m3fn) and scales [n_blocks, H_kv,
     2] float32, in place.  Returns (k_cache, v_cache, scales)."""
     _, dt, code = _of_floats(k, 3, "k")
-    torch, dev, cur = _current()
+    torch, dev, cur = _current(stream)
     kc, vc, sc, n_blocks, H_kv, d = _cache_arrays(k_cache, v_cache, scales, dev)
     T = k.shape[0]
     shape = (T, H_kv, d)
@@ -627,7 +632,7 @@ def saki_cache_write(k, v, slots, k_cache, v_cache, scales, stream=None):
     vp_, ldv = _rows(v, dt, shape, dev, "v")
     st = _args_mod.saki_cache_write(kp, vp_, code, T, H_kv, d, ldk, ldv,
                                     _array(slots, torch.int32, (T,), dev, "slots"), kc, vc, sc,
-                                    n_blocks, cur if stream is None else stream.cuda_stream)
+                                    n_blocks, cur)
     if st:
         _check("saki_cache_write", st)
     return k_cache, v_cache, scales
@@ -643,7 +648,7 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
     tables [B, max_blocks] and lens [B] int32, top_idx [B, H_q, Q, k] int32 (the
     listed keys only; none with k = 0) or None (every key).  Returns out, as q."""
     shape, dt, code = _of_floats(q, 4, "q")
-    torch, dev, cur = _current()
+    torch, dev, cur = _current(stream)
     B, H_q, Q, d = shape
     qp = _array(q, dt, shape, dev, "q")
     kc, vc, sc, n_blocks, H_kv, dc = _cache_arrays(k_cache, v_cache, scales, dev)
@@ -677,7 +682,7 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
             wp = _array(ws, torch.uint8, (wn,), dev, "ws")
     st = _args_mod.saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp,
                                      max_blocks, lp, ip, k, op, wp, wn,
-                                     cur if stream is None else stream.cuda_stream)
+                                     cur)
     if st:
         _check("saki_cache_attend", st)
     return out
@@ -692,7 +697,7 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
     causal attention within each of the packed prompts.  Returns out [T, H_q, d].
     ws: uint8 workspace (float32 only; allocated if not given)."""
     shape, dt, code = _of_floats(q, 3, "q")
-    torch, dev, cur = _current()
+    torch, dev, cur = _current(stream)
     T, H_q, d = shape
     H_kv = _heads(k, "k")
     kshape = (T, H_kv, d)
@@ -714,7 +719,7 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
         wp = _array(ws, torch.uint8, (wn,), dev, "ws")
     st = _args_mod.saki_attend_prompt(qp, kp, vp_, code, T, n - 1, H_q, H_kv, d, ldq, ldk, ldv, cp,
                                       _array(out, dt, shape, dev, "out"), wp, wn,
-                                      cur if stream is None else stream.cuda_stream)
+                                      cur)
     if st:
         _check("saki_attend_prompt", st)
     return out

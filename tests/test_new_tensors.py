@@ -48,3 +48,18 @@ def test_new_tensors_belong_to_the_stream_that_writes_them(monkeypatch):
     assert t.used_on == ["current"]  # the caller's, who reads it after waiting
     t = S._new(None, (3,), torch.uint8, "cuda:0")
     assert t.stream == "current" and t.used_on == []
+
+
+class Stream:
+    def __init__(self, device_index):
+        self.device_index, self.cuda_stream = device_index, 4096 + device_index
+
+
+def test_streams_of_another_device_are_refused(monkeypatch):
+    """The serving calls check that tensors lie on the current device, on which
+    kernels are launched and new tensors made: its streams alone are taken."""
+    monkeypatch.setattr(S, "_torch_mod", Torch())
+    monkeypatch.setattr(S, "_get_device", lambda: 0)
+    assert S._current(Stream(0))[1:] == (0, 4096)
+    with pytest.raises(ValueError, match="stream is on cuda:1"):
+        S._current(Stream(1))
