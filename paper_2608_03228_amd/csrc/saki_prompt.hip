@@ -621,13 +621,12 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = fmaxf(top, swap32(top)) * f;
-    // a key 2^100 below the row's largest weight is scaled no further up
-    float adds = fmaxf(mixed ? -INFINITY : top, fmaxf(m, top) - 100.f) - (float)ex.v;
+    float adds = top - (float)ex.v;
     if constexpr (mixed) {
-      float most = -INFINITY;
+      adds = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i] - (float)own_v(i));
-      adds = fmaxf(adds, fmaxf(most, swap32(most)));
+      for (int i = 0; i < 16; ++i) adds = fmaxf(adds, s[i] - (float)own_v(i));
+      adds = fmaxf(adds, swap32(adds));
     }
     if (__any(top > m + kSlack || adds > c + kRoom)) {
       const float m1 = fmaxf(m, top);
@@ -649,14 +648,8 @@ __global__ __launch_bounds__(256, 3 - KS) void prompt_attend_f32_kernel(PromptAr
       p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], f, shift));
       l += p[i];
     }
-    if constexpr (mixed) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = ldexp_f32(p[i], C - own_v(i));
-    } else {
-      const float part = ldexp_f32(1.f, C - ex.v);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] *= part;
-    }
+    for (int i = 0; i < 16; ++i) p[i] = ldexp_f32(p[i], C - (mixed ? own_v(i) : ex.v));  // (2^(C - e) may not be a float)
     f16x8_t ph[2], pl[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {

@@ -67,7 +67,7 @@ def test_rows_behind_a_sink(below, sink, heads):
 
 @pytest.mark.parametrize("heads", HEADS)
 @pytest.mark.parametrize("where", ["tile before", "key before", "key beside", "key behind"])
-@pytest.mark.parametrize("power", [10, 17, 28, 60])
+@pytest.mark.parametrize("power", [10, 17, 28, 60, 100, 122])
 def test_rows_beside_values_of_another_size(power, where, heads):
     """Keys without weight (2^-78 and less), or not seen, whose values are larger
     by many powers of two."""
@@ -106,4 +106,6 @@ def test_a_later_key_of_another_size_changes_no_row(heads):
     s, v = rng.standard_normal(1024), rng.standard_normal((1024, 128))
     s[100::97] = -200.0
     v[100::97] *= 2.0 ** 90
+    check(s, v, heads)
+    v[100::97] *= 2.0 ** 32
     check(s, v, heads)
