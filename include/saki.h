@@ -359,6 +359,9 @@ int saki_attend(const void* keys, int key_dtype, const float* values, const void
  *     code times the scale of its block and head.  H_kv * n_blocks < 2^25.
  *   - Lengths, tables and slots are read on the device.  Table entries, slots
  *     and list entries out of range are skipped, never followed.
+ *   - No token (T = 0), no query (Q = 0) and no prompt (B = 0 in
+ *     saki_attend_prompt) are fine and launch nothing; saki_block_tables and
+ *     saki_cache_attend take one request at least (SAKI_ERR_ARG).
  */
 enum {
   SAKI_CACHE_BLOCK = 64, /* tokens per cache block */

@@ -596,9 +596,10 @@ __device__ __forceinline__ Share share_of(long long total, int groups) {
 // terms, three for float32 output) are split so that nothing but the output is
 // rounded to bf16.  HBM bound, 16 KB a tile: 8 requests of up to 131,072 keys in
 // 4 heads in 108 us, 5.5 TB/s of 590 MB fetched.  A request of 4,001 keys in 8
-// heads takes 10.2 us, and the join 4.4: a chain of reads (lengths, table, codes)
-// with a tile a wave behind it.  Holding the next tile's codes in registers
-// (241 of them) did not shorten either, 14.2 us against 13.4 for the step.
+// heads takes 9.5-10.2 us, and the join 4.2-4.8 (in a kernel trace; 13.4 as calls
+// in a row): a chain of reads (lengths, table, codes) with a tile a
+// wave behind it.  Holding the next tile's codes in registers (241 of them) did
+// not shorten either, 14.2 us against 13.4 for the step.
 //
 // Without SPLIT a work-group takes one whole pair: no share to find, no
 // workspace and no join (see whole_better).
@@ -836,8 +837,10 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
 
 // Joins the parts of the pairs that several work-groups shared, and writes
 // zeros for requests without a key.  A work-group takes 16 dims of a pair (all
-// dims, 16 at a time, where there are many pairs); its four waves take every
-// fourth part.
+// dims, 16 at a time, above 256 pairs); its four waves take every fourth part.
+// us of attention and join, a group a pair / eight (bf16, 32 / 8 heads, tables of
+// 40 and 80 tiles): 128 pairs 26.1 / 19.3, 256 34.0 / 30.3, 320 50.4 / 47.2, 512
+// 89.1 / 88.3, 1,024 148 / 153, 4,096 524 / 562.
 template <bool F32>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups, const float* __restrict__ ws,
                                                          void* out) {
@@ -915,8 +918,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups
 // Attention over listed keys: one wave per (request, head, query) row.  Lane e
 // looks up entry e; eight lanes then read one key's or value's 128 bytes, eight
 // entries at a time, all in flight together.  Few rows are latency bound (list,
-// table, codes): 256 over 131,072 keys take 7.7 us, 8.4 with four of the waves a
-// work-group, on a quarter of the CUs; 32,768 rows read 5.4 TB/s.
+// table, codes): 256 over 131,072 keys take 7.2-7.7 us as calls in a row (8.4-8.6
+// in a kernel trace), 8.4 with four of the waves a work-group, on a quarter
+// of the CUs; 32,768 rows read 5.4 TB/s.
 template <bool F32>
 __global__ __launch_bounds__(64) void cache_lists_kernel(CacheArgs a, const void* __restrict__ q,
                                                           const int* __restrict__ top_idx, int k,
@@ -1139,8 +1143,9 @@ int saki_cache_write(const void* k, const void* v, int dtype, int T, int H_kv, i
 namespace {
 
 // Whether a work-group takes a whole pair: the lengths are read on the device,
-// so the tables' width has to bound a group's time.  us (bf16, 32 / 8 heads),
-// split and joined / whole pairs, for requests of the full width:
+// so the tables' width has to bound a group's time.  us (bf16, 32 / 8 heads, calls
+// in a row in a graph), split and joined / whole pairs, for requests of the full
+// width:
 //                4 tiles       8            12           16           32           64
 //    1 request   8.1 / 5.7    9.4 / 7.6    9.3 / 9.2    9.5 / 10.8  10.0 / 17.2  10.8 / 29.6
 //    8           8.4 / 5.8    9.7 / 7.7    9.8 / 9.3   10.0 / 10.9  13.2 / 18.8
@@ -1148,6 +1153,16 @@ namespace {
 //   32                       14.2 / 8.5                20.8 / 14.7  30.6 / 23.3
 //   64          12.7 / 8.2   18.7 / 14.3               29.1 / 24.7  49.3 / 44.0   106 / 99
 //  256          34.1 / 26.2                             108 / 100    193 / 192
+// float32, later, with lengths of the full width, and with any up to it:
+//    1 request   9.2 / 6.4   10.2 / 8.5   10.3 / 10.5  10.3 / 12.4  10.8 / 20.8
+//    8                       10.8 / 8.6   11.4 / 10.6  12.0 / 14.3  15.4 / 24.1
+//    8, any                  13.8 / 8.6   13.8 / 10.5  21.1 / 12.5  17.3 / 23.2
+//   16                                                 15.3 / 15.1  20.1 / 24.5
+//   32                                                 21.0 / 16.0  31.0 / 27.1  61.8 / 63.9
+//   32, any                                            29.7 / 14.9  43.9 / 24.4  55.0 / 54.4
+//   64                                                 28.2 / 24.7  57.1 / 53.1   104 / 100
+//   64, any                                            50.4 / 20.5  63.0 / 37.8  97.0 / 73.5
+//  256          40.4 / 34.3                             114 / 105    209 / 200
 // (many pairs fill the GPU without being split, up to the width where one long
 // request among short ones would keep its groups at work alone for long).
 bool whole_better(long long pairs, int max_blocks) {
