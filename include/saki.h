@@ -348,7 +348,10 @@ int saki_attend(const void* keys, int key_dtype, const float* values, const void
  *
  *   - d is 128.  Queries, keys, values and outputs are float32 or bf16
  *     (`dtype`, the same for all of a call), rounded to nearest even where they
- *     are written; scores, softmax, sums and scales are float32.
+ *     are written; scores, softmax, sums and scales are float32.  An attention's
+ *     sums are of weights up to one (saki_attend_prompt in bf16: 2^8) times
+ *     values, divided at the end: values of more than 2^128 / (256 keys) may
+ *     overflow them.
  *   - Token rows [T, H, d] may lie ld elements apart (ld >= H * d, dense heads
  *     within a row: slices of a fused projection).  Such pointers, queries and
  *     outputs are 16-byte aligned, and ld * (size of an element) is a multiple
