@@ -237,18 +237,19 @@ def _stream(stream):
     return _torch().cuda.current_stream().cuda_stream
 
 
-def _new(stream, shape, dtype, dev):
+def _new(stream, shape, dtype, dev, result=True):
     """A tensor that the call writes or works in, of the memory of the stream
     that does: what the current stream's pool hands out may still be in use by
     what is queued there, which a call on another stream does not wait for.
-    Marked as used on the current stream too, whose work reads it next."""
+    A result is marked as used on the current stream too, whose work reads it
+    next; a workspace is not, so that its stream's next call can have it."""
     torch = _torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=dev)
     here = torch.cuda.current_stream(dev)
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=dev)
-    if here != stream:
+    if result and here != stream:
         t.record_stream(here)
     return t
 
@@ -327,7 +328,7 @@ def saki_score_topk(index, sketch: str, q, B_q, mu, H_kv: int, N_cap: int, N_val
     if ws is None or not _plain(N_valid, r, k):
         need = saki_score_topk_workspace_bytes(B, H_q, Q, N_valid, r, k, sketch, ih)
     if ws is None:
-        ws = _new(stream, max(need, 1), torch.uint8, q.device)
+        ws = _new(stream, max(need, 1), torch.uint8, q.device, result=False)
     if top_idx is None:
         top_idx = _new(stream, (B, H_q, Q, k), torch.int32, q.device)
     if with_scores and top_score is None:
@@ -380,7 +381,7 @@ def saki_recall(keys, q, approx_idx, N_valid: int, q_pos=None, k: int = 64, ws=N
     if ws is None or not _plain(N_valid, k):
         need = saki_recall_workspace_bytes(B, H_q, H_kv, Q, N_valid, d, k)
     if ws is None:
-        ws = _new(stream, max(need, 1), torch.uint8, q.device)
+        ws = _new(stream, max(need, 1), torch.uint8, q.device, result=False)
     if hits is None:
         hits = _new(stream, (B, H_q, Q), torch.int32, q.device)
     if want_exact and exact_idx is None:
@@ -668,7 +669,7 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
         k = top_idx.shape[-1]
         ip = _array(top_idx, torch.int32, (B, H_q, Q, k), dev, "top_idx")
         if k == 0:  # lists of nothing: as lists of one entry that names no key
-            top_idx = _new(stream, (B, H_q, Q, 1), torch.int32, q.device)
+            top_idx = _new(stream, (B, H_q, Q, 1), torch.int32, q.device, result=False)
             with torch.cuda.stream(stream):
                 top_idx.fill_(-1)
             k, ip = 1, top_idx.data_ptr()
@@ -676,7 +677,7 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
         if ws is None:
             need = _args_mod.saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, 0)
             if need > NO_WORKSPACE:
-                ws = _new(stream, need, torch.uint8, q.device)
+                ws = _new(stream, need, torch.uint8, q.device, result=False)
         if ws is not None:
             wn = ws.numel()
             wp = _array(ws, torch.uint8, (wn,), dev, "ws")
@@ -713,7 +714,7 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
     wp, wn = None, 0
     if ws is None and code == F32:
         need = _args_mod.saki_attend_prompt_workspace_bytes(F32, T, n - 1, H_kv)
-        ws = _new(stream, max(need, 1), torch.uint8, q.device)
+        ws = _new(stream, max(need, 1), torch.uint8, q.device, result=False)
     if ws is not None:
         wn = ws.numel()
         wp = _array(ws, torch.uint8, (wn,), dev, "ws")

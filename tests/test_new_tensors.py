@@ -46,6 +46,8 @@ def test_new_tensors_belong_to_the_stream_that_writes_them(monkeypatch):
     t = S._new("side", (3,), torch.uint8, "cuda:0")
     assert t.stream == "side" and fake.now == "current"
     assert t.used_on == ["current"]  # the caller's, who reads it after waiting
+    t = S._new("side", (3,), torch.uint8, "cuda:0", result=False)
+    assert t.stream == "side" and t.used_on == []  # no other stream keeps a workspace back
     t = S._new(None, (3,), torch.uint8, "cuda:0")
     assert t.stream == "current" and t.used_on == []
 
