@@ -16,7 +16,9 @@
  *
  * Beside the index: saki_attend (attention over its lists) and what a server
  * runs around it (saki_rope, saki_block_tables, saki_cache_write,
- * saki_cache_attend, saki_attend_prompt; "Serving around the index" below).
+ * saki_cache_attend, saki_attend_prompt; "Serving around the index" below), with
+ * a cache held in 4 bits (saki_cache4_write, saki_cache4_read,
+ * saki_cache4_attend, saki_cache4_prompt; "A cache held in 4 bits").
  *
  * Conventions shared by every entry point
  *   - Return value: SAKI_OK (0) or a negative saki_status; nothing throws.
@@ -494,6 +496,103 @@ size_t saki_attend_prompt_workspace_bytes(int dtype, int T, int B, int H_kv);
  */
 int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, int T, int B,
                        int H_q, int H_kv, int d, size_t ld_q, size_t ld_k, size_t ld_v,
+                       const int* cu, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A cache held in 4 bits: 136 bytes a token and KV head (the 8-bit cache: 256),
+ * with the same blocks, tables, slots and lists, and what is said above of types,
+ * token rows, lengths and what is out of range.
+ *
+ *   - An element is an E2M1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; OCP
+ *     4-bit floats) times the scale of its group of 32 dims of the token, a power
+ *     of two held as an E8M0 byte e: 2^(e - 127).  e is 27 to 247, or 255: the
+ *     group's elements are NaN.
+ *   - k_cache, v_cache: device [n_blocks, H_kv, 64, 64] bytes, two codes a byte,
+ *     the even dim's in the low half.  Byte i (dims 2 i, 2 i + 1) of block token t
+ *     is at 64 t + i for keys, at 256 (t / 4) + 16 (i / 4) + 4 (t % 4) + i % 4 for
+ *     values.
+ *   - scales: device [n_blocks, H_kv, 2 (keys, values), 64 (tokens), 4 (groups)]
+ *     bytes.  All three are 16-byte aligned; H_kv * n_blocks < 2^25.
+ */
+
+/*
+ * saki_cache4_write (GPU) -- keys and values of T tokens to their slots, as the
+ * nearest codes (ties to the even code, the sign of zero kept) under the scale of
+ * their group: the least power of two s, at least 2^-100, with |x| <= 7 s for its
+ * 32 elements.  Elements above 6 s become 6 s, half a step away at most; s is no
+ * more than 2^120, above which they become 6 s too.  A group with an element that
+ * is not finite is held as NaN.
+ *
+ *   k, v     device [T, H_kv, d], rows ld_k, ld_v apart, apart from the caches
+ *   slots    device int [T], distinct (what a slot given twice then holds is not
+ *            specified); tokens with slots out of range are skipped
+ * Other slots are left as they were.  T <= 2^26.  SAKI_ERR_ARG where the caches
+ * and scales overlap.
+ */
+int saki_cache4_write(const void* k, const void* v, int dtype, int T, int H_kv, int d,
+                      size_t ld_k, size_t ld_v, const int* slots, void* k_cache, void* v_cache,
+                      void* scales, int n_blocks, void* stream);
+
+/*
+ * saki_cache4_read (GPU) -- ranges of the requests' tokens as float32 or bf16 rows
+ * (both hold them exactly): rows [cu[b], cu[b+1]) of the outputs are request b's
+ * tokens from starts[b] on, say a step's new tokens (cu of saki_block_tables, its
+ * ctx_lens as starts) or whole contexts (starts NULL: from token 0).
+ *
+ *   tables  device int [B, max_blocks]
+ *   starts  device int [B], or NULL;  cu  device int [B + 1], ascending
+ *   k_out, v_out  device [T, H_kv, d], rows ld_k, ld_v apart; either may be NULL
+ * A token without a block in its table reads as zeros; rows of no request are
+ * left as they were.  T <= 2^26.  The outputs overlap neither each other nor an
+ * input.
+ */
+int saki_cache4_read(const void* k_cache, const void* v_cache, const void* scales, int n_blocks,
+                     const int* tables, int max_blocks, const int* starts, const int* cu, int B,
+                     int T, int H_kv, int d, int dtype, void* k_out, void* v_out, size_t ld_k,
+                     size_t ld_v, void* stream);
+
+/* Workspace for saki_cache4_attend (bytes; 0 on bad arguments), as for
+ * saki_cache_attend. */
+size_t saki_cache4_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int max_blocks, int k);
+
+/*
+ * saki_cache4_attend (GPU) -- saki_cache_attend over the 4-bit cache: attention of
+ * the Q newest tokens' queries per request and head, over every key that they see
+ * or, with top_idx, over the listed ones.  The arguments are those of
+ * saki_cache_attend.  Elements and their scales enter the products exactly.  A NaN
+ * group makes the rows that see it NaN (a value's in its dims), and no others.
+ */
+int saki_cache4_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q, int d,
+                       const void* k_cache, const void* v_cache, const void* scales, int n_blocks,
+                       const int* tables, int max_blocks, const int* lens, const int* top_idx,
+                       int k, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace for saki_cache4_prompt (bytes; 0 on bad arguments): the parts of rows
+ * whose keys several work-groups share. */
+size_t saki_cache4_prompt_workspace_bytes(int T, int B, int H_q, int H_kv, int max_blocks);
+
+/*
+ * saki_cache4_prompt (GPU) -- causal attention of packed chunks of new tokens over
+ * the 4-bit cache that already holds them (saki_cache4_write before): token i of
+ * the cu[b+1] - cu[b] of request b stands at position lens[b] - (cu[b+1] - cu[b])
+ * + i and attends over the request's keys up to there, every query head over the
+ * keys of its group.  A whole prompt, a chunk of a long one and a follow-up to a
+ * conversation differ in lens alone.  A row without a key writes zeros.  bf16
+ * queries meet the elements in exact products and weights are rounded to bf16 for
+ * theirs; float32 queries and weights are taken as three bf16 terms (2^-25 of
+ * them is left out).
+ *
+ *   q       device [T, H_q, d] rows ld_q apart
+ *   tables  device int [B, max_blocks];  lens  device int [B], the new tokens counted
+ *   cu      device int [B + 1], ascending
+ *   out     device [T, H_q, d], dense, overlaps no input; tokens of no request are
+ *           left as they were
+ *   ws      device workspace of saki_cache4_prompt_workspace_bytes(...), 16-byte
+ *           aligned
+ */
+int saki_cache4_prompt(const void* q, int dtype, int T, int B, int H_q, int H_kv, int d,
+                       size_t ld_q, const void* k_cache, const void* v_cache, const void* scales,
+                       int n_blocks, const int* tables, int max_blocks, const int* lens,
                        const int* cu, void* out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus

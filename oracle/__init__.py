@@ -16,5 +16,7 @@ from .saki import *  # noqa: F401,F403
 from .saki import __all__  # noqa: F401
 from .serve import *  # noqa: F401,F403
 from .serve import __all__ as _serve_all
+from .cache4 import *  # noqa: F401,F403
+from .cache4 import __all__ as _cache4_all
 
-__all__ = __all__ + _serve_all
+__all__ = __all__ + _serve_all + _cache4_all

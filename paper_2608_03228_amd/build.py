@@ -23,7 +23,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
-KERNELS = ("saki_kernels", "saki_serve", "saki_prompt")  # the index, and serving around it
+KERNELS = ("saki_kernels", "saki_serve", "saki_prompt",  # the index, and serving around it
+           "saki_cache4", "saki_chunk4")  # a cache held in 4 bits
 # Packed FP32 instructions are disabled for all device code.
 NO_PACKED_FP32 = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # MFMA results are written to the architectural VGPRs rather than the

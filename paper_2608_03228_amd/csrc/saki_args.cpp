@@ -168,6 +168,12 @@ PyMethodDef methods[] = {
     SAKI_ENTRY(saki_cache_attend_workspace_bytes),
     SAKI_ENTRY(saki_attend_prompt),
     SAKI_ENTRY(saki_attend_prompt_workspace_bytes),
+    SAKI_ENTRY(saki_cache4_write),
+    SAKI_ENTRY(saki_cache4_read),
+    SAKI_ENTRY(saki_cache4_attend),
+    SAKI_ENTRY(saki_cache4_attend_workspace_bytes),
+    SAKI_ENTRY(saki_cache4_prompt),
+    SAKI_ENTRY(saki_cache4_prompt_workspace_bytes),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -75,6 +75,15 @@ def lib():
         "saki_attend_prompt": (ip, [vp, vp, vp, ip, ip, ip, ip, ip, ip, sz, sz, sz, vp, vp, vp,
                                     sz, vp]),
         "saki_attend_prompt_workspace_bytes": (sz, [ip, ip, ip, ip]),
+        "saki_cache4_write": (ip, [vp, vp, ip, ip, ip, ip, sz, sz, vp, vp, vp, vp, ip, vp]),
+        "saki_cache4_read": (ip, [vp, vp, vp, ip, vp, ip, vp, vp, ip, ip, ip, ip, ip, vp, vp, sz,
+                                  sz, vp]),
+        "saki_cache4_attend_workspace_bytes": (sz, [ip, ip, ip, ip, ip, ip]),
+        "saki_cache4_attend": (ip, [vp, ip, ip, ip, ip, ip, ip, vp, vp, vp, ip, vp, ip, vp, vp, ip,
+                                    vp, vp, sz, vp]),
+        "saki_cache4_prompt_workspace_bytes": (sz, [ip, ip, ip, ip, ip]),
+        "saki_cache4_prompt": (ip, [vp, ip, ip, ip, ip, ip, ip, sz, vp, vp, vp, ip, vp, ip, vp, vp,
+                                    vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -648,11 +657,16 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
     """q [B, H_q, Q, d] (float32 or bfloat16), the cache of saki_cache_write,
     tables [B, max_blocks] and lens [B] int32, top_idx [B, H_q, Q, k] int32 (the
     listed keys only; none with k = 0) or None (every key).  Returns out, as q."""
+    return _attend_cached("saki_cache_attend", _cache_arrays, q, (k_cache, v_cache, scales), tables,
+                          lens, top_idx, out, ws, stream)
+
+
+def _attend_cached(name, arrays, q, cache, tables, lens, top_idx, out, ws, stream):
     shape, dt, code = _of_floats(q, 4, "q")
     torch, dev, cur = _current(stream)
     B, H_q, Q, d = shape
     qp = _array(q, dt, shape, dev, "q")
-    kc, vc, sc, n_blocks, H_kv, dc = _cache_arrays(k_cache, v_cache, scales, dev)
+    kc, vc, sc, n_blocks, H_kv, dc = arrays(*cache, dev)
     if dc != d:
         raise ValueError(f"q has d = {d}, the cache {dc}")
     if tables.dim() != 2:
@@ -675,17 +689,16 @@ def saki_cache_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, o
             k, ip = 1, top_idx.data_ptr()
     else:
         if ws is None:
-            need = _args_mod.saki_cache_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, 0)
+            need = getattr(_args_mod, name + "_workspace_bytes")(B, H_q, H_kv, Q, max_blocks, 0)
             if need > NO_WORKSPACE:
                 ws = _new(stream, need, torch.uint8, q.device, result=False)
         if ws is not None:
             wn = ws.numel()
             wp = _array(ws, torch.uint8, (wn,), dev, "ws")
-    st = _args_mod.saki_cache_attend(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp,
-                                     max_blocks, lp, ip, k, op, wp, wn,
-                                     cur)
+    st = getattr(_args_mod, name)(qp, code, B, H_q, H_kv, Q, d, kc, vc, sc, n_blocks, tp,
+                                  max_blocks, lp, ip, k, op, wp, wn, cur)
     if st:
-        _check("saki_cache_attend", st)
+        _check(name, st)
     return out
 
 
@@ -723,4 +736,122 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
                                       cur)
     if st:
         _check("saki_attend_prompt", st)
+    return out
+
+
+# ------------------------------------------------------------------ a cache held in 4 bits
+
+def _cache4_arrays(k_cache, v_cache, scales, dev):
+    """-> pointers, n_blocks, H_kv, d"""
+    u8 = _torch().uint8
+    shape = k_cache.shape
+    if len(shape) != 4 or shape[2] != CACHE_BLOCK:
+        raise ValueError(f"k_cache must be [n_blocks, H_kv, {CACHE_BLOCK}, d / 2]")
+    n_blocks, H_kv, _, half = shape
+    return (_array(k_cache, u8, shape, dev, "k_cache"), _array(v_cache, u8, shape, dev, "v_cache"),
+            _array(scales, u8, (n_blocks, H_kv, 2, CACHE_BLOCK, half // 16), dev, "scales"),
+            n_blocks, H_kv, 2 * half)
+
+
+def saki_cache4_write(k, v, slots, k_cache, v_cache, scales, stream=None):
+    """k, v [T, H_kv, d] (float32 or bfloat16), slots [T] int32 (distinct), to
+    k_cache and v_cache [n_blocks, H_kv, 64, d / 2] and scales [n_blocks, H_kv, 2,
+    64, d / 32] (all uint8), in place.  Returns (k_cache, v_cache, scales)."""
+    _, dt, code = _of_floats(k, 3, "k")
+    torch, dev, cur = _current(stream)
+    kc, vc, sc, n_blocks, H_kv, d = _cache4_arrays(k_cache, v_cache, scales, dev)
+    T = k.shape[0]
+    shape = (T, H_kv, d)
+    kp, ldk = _rows(k, dt, shape, dev, "k")
+    vp_, ldv = _rows(v, dt, shape, dev, "v")
+    st = _args_mod.saki_cache4_write(kp, vp_, code, T, H_kv, d, ldk, ldv,
+                                     _array(slots, torch.int32, (T,), dev, "slots"), kc, vc, sc,
+                                     n_blocks, cur)
+    if st:
+        _check("saki_cache4_write", st)
+    return k_cache, v_cache, scales
+
+
+def saki_cache4_read(k_cache, v_cache, scales, tables, cu, k_out, v_out, starts=None, stream=None):
+    """The cache of saki_cache4_write, tables [B, max_blocks], cu [B + 1] and
+    starts [B] (None: 0) int32: request b's tokens from starts[b] on to rows
+    [cu[b], cu[b + 1]) of k_out and v_out [T, H_kv, d] (float32 or bfloat16; one of
+    them may be None).  Returns (k_out, v_out)."""
+    x, name = (v_out, "v_out") if k_out is None else (k_out, "k_out")
+    shape, dt, code = _of_floats(x, 3, name)
+    torch, dev, cur = _current(stream)
+    kc, vc, sc, n_blocks, H_kv, d = _cache4_arrays(k_cache, v_cache, scales, dev)
+    T = shape[0]
+    shape = (T, H_kv, d)
+    n = cu.shape[0] if cu.dim() == 1 else 0
+    if n < 1 or tables.dim() != 2:
+        raise ValueError("cu must be [B + 1] and tables [B, max_blocks]")
+    B, max_blocks = n - 1, tables.shape[1]
+    kp = vp_ = sp = None
+    ldk = ldv = 0
+    if k_out is not None:
+        kp, ldk = _rows(k_out, dt, shape, dev, "k_out")
+    if v_out is not None:
+        vp_, ldv = _rows(v_out, dt, shape, dev, "v_out")
+    if starts is not None:
+        sp = _array(starts, torch.int32, (B,), dev, "starts")
+    st = _args_mod.saki_cache4_read(kc, vc, sc, n_blocks,
+                                    _array(tables, torch.int32, (B, max_blocks), dev, "tables"),
+                                    max_blocks, sp, _array(cu, torch.int32, (n,), dev, "cu"), B, T,
+                                    H_kv, d, code, kp, vp_, ldk, ldv, cur)
+    if st:
+        _check("saki_cache4_read", st)
+    return k_out, v_out
+
+
+def saki_cache4_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, k=0) -> int:
+    return int(lib().saki_cache4_attend_workspace_bytes(B, H_q, H_kv, Q, max_blocks, k))
+
+
+def saki_cache4_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, out=None, ws=None,
+                       stream=None):
+    """saki_cache_attend over the cache of saki_cache4_write."""
+    return _attend_cached("saki_cache4_attend", _cache4_arrays, q, (k_cache, v_cache, scales),
+                          tables, lens, top_idx, out, ws, stream)
+
+
+def saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks) -> int:
+    return int(lib().saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks))
+
+
+def saki_cache4_prompt(q, k_cache, v_cache, scales, tables, lens, cu, out=None, ws=None,
+                       stream=None):
+    """q [T, H_q, d] (float32 or bfloat16), the cache of saki_cache4_write, tables
+    [B, max_blocks], lens [B] and cu [B + 1] int32: causal attention of the newest
+    cu[b + 1] - cu[b] of each request's lens[b] cached tokens over all of them.
+    Returns out [T, H_q, d].  ws: uint8 workspace (allocated if not given)."""
+    shape, dt, code = _of_floats(q, 3, "q")
+    torch, dev, cur = _current(stream)
+    T, H_q, d = shape
+    qp, ldq = _rows(q, dt, shape, dev, "q")
+    kc, vc, sc, n_blocks, H_kv, dc = _cache4_arrays(k_cache, v_cache, scales, dev)
+    if dc != d:
+        raise ValueError(f"q has d = {d}, the cache {dc}")
+    n = cu.shape[0] if cu.dim() == 1 else 0
+    if n < 1 or tables.dim() != 2:
+        raise ValueError("cu must be [B + 1] and tables [B, max_blocks]")
+    B, max_blocks = n - 1, tables.shape[1]
+    tp = _array(tables, torch.int32, (B, max_blocks), dev, "tables")
+    lp = _array(lens, torch.int32, (B,), dev, "lens")
+    cp = _array(cu, torch.int32, (n,), dev, "cu")
+    if out is None:
+        out = _new(stream, shape, dt, q.device)
+    wp, wn = None, 0
+    if ws is None:
+        need = _args_mod.saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks)
+        if need > NO_WORKSPACE:
+            ws = _new(stream, need, torch.uint8, q.device, result=False)
+    if ws is not None:
+        wn = ws.numel()
+        wp = _array(ws, torch.uint8, (wn,), dev, "ws")
+    st = _args_mod.saki_cache4_prompt(qp, code, T, B, H_q, H_kv, d, ldq, kc, vc, sc, n_blocks, tp,
+                                      max_blocks, lp, cp, _array(out, dt, shape, dev, "out"), wp, wn,
+                                      cur)
+    if st:
+        _check("saki_cache4_prompt", st)
     return out
