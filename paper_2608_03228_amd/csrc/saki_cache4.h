@@ -45,16 +45,18 @@ __device__ __forceinline__ uint32_t encode8(const float* x, float s) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6], x[7], s, 3);
 }
 
-// Eight codes times their scale: exact in bf16 (2 significant bits).
+// Two codes (byte B of four) times their scale: exact in bf16 (2 significant bits).
+template <int B>
+__device__ __forceinline__ uint32_t decode2(uint32_t c, float s) {
+  const bf16x2_t v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, B);
+  uint32_t r;
+  __builtin_memcpy(&r, &v, 4);
+  return r;
+}
+// Eight codes times their scale.
 __device__ __forceinline__ void decode8(uint32_t c, float s, uint32_t* pairs) {
-  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0);
-  const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1);
-  const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2);
-  const bf16x2_t e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
-  __builtin_memcpy(&pairs[0], &a, 4);
-  __builtin_memcpy(&pairs[1], &b, 4);
-  __builtin_memcpy(&pairs[2], &d, 4);
-  __builtin_memcpy(&pairs[3], &e, 4);
+  pairs[0] = decode2<0>(c, s), pairs[1] = decode2<1>(c, s);
+  pairs[2] = decode2<2>(c, s), pairs[3] = decode2<3>(c, s);
 }
 __device__ __forceinline__ void decode8(uint32_t c, float s, float* x) {
   const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0);

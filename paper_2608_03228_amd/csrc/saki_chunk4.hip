@@ -180,12 +180,15 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
       }
       const float shift = m == -INFINITY ? 0.f : -m * (kScale * kLog2e);  // (a row that sees none of the keys yet)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b) {
+        float sum = 0.f;  // (a sum of sums: a row's N / 2 weights one by one would lose 2^-24 sqrt(N) of it)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], kScale * kLog2e, shift));
-          l += s[b][i];
+          sum += s[b][i];
         }
+        l += sum;
+      }
 #pragma unroll
       for (int y = 0; y < 2 * NB; ++y) {  // 16 keys each
         float p[8];

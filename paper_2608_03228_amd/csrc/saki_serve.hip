@@ -674,6 +674,86 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(CacheArgs a, const
   }
 }
 
+// Joins the parts of the pairs that several work-groups shared, and writes
+// zeros for requests without a key.  A work-group takes 16 dims of a pair (all
+// dims, 16 at a time, above 256 pairs); its four waves take every fourth part.
+// us of attention and join, a group a pair / eight (bf16, 32 / 8 heads, tables of
+// 40 and 80 tiles): 128 pairs 26.1 / 19.3, 256 34.0 / 30.3, 320 50.4 / 47.2, 512
+// 89.1 / 88.3, 1,024 148 / 153, 4,096 524 / 562.
+template <bool F32>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheArgs a, int groups, const float* __restrict__ ws,
+                                                         void* out) {
+  __shared__ long long part[4], s_base;
+  __shared__ float s_m[4][16], s_l[4][16], s_y[4][16][16];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int G = a.H_q / a.H_kv, R = G * a.Q, RB = (R + 15) / 16, pairs = a.H_kv * RB;
+  const int b = blockIdx.x / pairs, pair = blockIdx.x % pairs;
+  long long total = 0, base;
+  int nt;
+  if (a.B <= kWave) {
+    const Sums all = wave_sums(a);
+    total = (long long)all.total * pairs;
+    nt = __builtin_amdgcn_readlane(all.mine, b);
+    base = (long long)(__builtin_amdgcn_readlane(all.upto, b) - nt) * pairs;
+  } else {
+    for (int b0 = 0; b0 < a.B; b0 += 256) {
+      const int t = b0 + tid < a.B ? tiles_of(a.lens[b0 + tid], a.max_blocks) : 0;
+      long long sum;
+      const long long upto = group_scan((long long)t * pairs, part, &sum);
+      if (b0 + tid == b) s_base = total + upto - (long long)t * pairs;
+      total += sum;
+    }
+    __syncthreads();
+    nt = tiles_of(a.lens[b], a.max_blocks);
+    base = s_base;
+  }
+  const Share sh = share_of(total, groups);
+  const long long from = base + (long long)nt * pair;
+  const int w0 = (int)(from / sh.piece), w1 = nt ? (int)((from + nt - 1) / sh.piece) : w0;
+  if (nt && w0 == w1) return;
+  const int row = lane / 4;
+  const int hk = pair / RB, r0 = pair % RB * 16;
+  const bool in = r0 + row < R;
+  for (int part16 = blockIdx.y; part16 < kHeadDim / 16; part16 += gridDim.y) {
+    const int d0 = part16 * 16 + lane % 4 * 4;
+    float M = -INFINITY, L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    if (nt && in)
+      for (int w = w0 + wave; w <= w1; w += 4) {
+        const float* p = ws + ((size_t)w * 2 + (w == w0)) * kPartFloats;
+        const float m = p[kPartRows * kHeadDim + row], l = p[kPartRows * kHeadDim + kPartRows + row];
+        const float4 x = *reinterpret_cast<const float4*>(p + row * kHeadDim + d0);
+        const float m1 = fmaxf(M, m), ref = m1 == -INFINITY ? 0.f : m1;
+        const float e0 = __builtin_amdgcn_exp2f(M - ref), e1 = __builtin_amdgcn_exp2f(m - ref);
+        M = m1;
+        L = L * e0 + l * e1;
+        y[0] = y[0] * e0 + x.x * e1, y[1] = y[1] * e0 + x.y * e1;
+        y[2] = y[2] * e0 + x.z * e1, y[3] = y[3] * e0 + x.w * e1;
+      }
+    __syncthreads();  // the last dims are read
+    s_m[wave][row] = M, s_l[wave][row] = L;  // equal from a row's four lanes
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s_y[wave][row][lane % 4 * 4 + j] = y[j];
+    __syncthreads();
+    const int r = tid / 16, d = tid % 16;
+    if (r0 + r >= R) continue;
+    M = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+    float sum = 0.f;
+    L = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float e = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - M);
+      L += s_l[w][r] * e;
+      sum += s_y[w][r][d] * e;
+    }
+    sum = L == 0.f ? 0.f : sum / L;  // (a NaN stays one)
+    const size_t to = (((size_t)b * a.H_q + (size_t)hk * G) * a.Q + r0 + r) * kHeadDim + part16 * 16 + d;
+    if constexpr (F32)
+      ((float*)out)[to] = sum;
+    else
+      ((__bf16*)out)[to] = (__bf16)sum;
+  }
+}
+
 // Attention over listed keys: one wave per (request, head, query) row.  Lane e
 // looks up entry e; eight lanes then read one key's or value's 128 bytes, eight
 // entries at a time, all in flight together.  Few rows are latency bound (list,
