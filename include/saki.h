@@ -568,8 +568,9 @@ int saki_cache4_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q
                        int k, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /* Workspace for saki_cache4_prompt (bytes; 0 on bad arguments): the parts of rows
- * whose keys several work-groups share. */
-size_t saki_cache4_prompt_workspace_bytes(int T, int B, int H_q, int H_kv, int max_blocks);
+ * whose keys several work-groups share, at most 140 MB. */
+size_t saki_cache4_prompt_workspace_bytes(int dtype, int T, int B, int H_q, int H_kv,
+                                          int max_blocks);
 
 /*
  * saki_cache4_prompt (GPU) -- causal attention of packed chunks of new tokens over

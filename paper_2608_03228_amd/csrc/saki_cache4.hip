@@ -13,40 +13,55 @@ namespace {
 
 // ---------------------------------------------------------------- writing
 
-// A wave takes four tokens of one head's keys or values, 16 lanes a token and 8
-// dims a lane; four lanes hold a group and find its largest element.  Four tokens
-// whose slots stand together fill 256 contiguous bytes of codes, in either
-// layout.  Groups have their own scales, so that nothing there before is read.
+// A wave takes eight tokens of one head's keys or values, four at a time, 16 lanes
+// a token and 8 dims a lane; four lanes hold a group and find its largest element.
+// Four tokens whose slots stand together fill 256 contiguous bytes of codes, in
+// either layout.  Groups have their own scales, so that nothing there before is
+// read.  HBM bound on prompts: 30,400 float32 tokens of 4 heads in 31 us, 4.6 TB/s;
+// bf16 in 17.1 (20.3 with four tokens a wave and their loads behind the slots').
+constexpr int kWriteTokens = 8;  // of a wave
 template <typename T>
 __global__ __launch_bounds__(256) void cache4_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
                                                            size_t ld_k, size_t ld_v, int n_tokens,
                                                            const int* __restrict__ slots, int n_blocks, int H,
                                                            uint8_t* k_cache, uint8_t* v_cache, uint8_t* scales) {
+  constexpr int U = kWriteTokens / 4;
   const int lane = threadIdx.x % kWave;
   const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
-  const uint32_t quad = item / (2 * H), hw = item % (2 * H);
+  const uint32_t quad = item / (2 * H) * U, hw = item % (2 * H);
   const int which = hw >= (uint32_t)H, h = which ? hw - H : hw;
-  const uint32_t t = quad * 4 + lane / 16;
   const int m = lane % 16;
-  const int slot = t < (uint32_t)n_tokens ? slots[t] : -1;
-  const bool in = slot >= 0 && slot < n_blocks * kTile;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (in) load_elems<T, 8>((which ? v + t * ld_v : k + t * ld_k) + (size_t)h * kHeadDim + 8 * m, x);
-  uint32_t top = 0;
+  int slot[U];
+  float x[U][8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max(top, xor_shfl_u32(top, 1));
-  top = max(top, xor_shfl_u32(top, 2));
-  const uint32_t byte = scale_byte(top);
-  const uint32_t codes = encode8(x, scale_of(byte));
-  if (!in) return;
-  const size_t at = (size_t)(slot / kTile) * H + h;
-  const int token = slot % kTile;
-  *reinterpret_cast<uint32_t*>((which ? v_cache : k_cache) + at * kCodes4 + code_at(which, token, m)) = codes;
-  if (m % 4 == 0) scales[at * kScales4 + (which * kTile + token) * kGroups4 + m / 4] = (uint8_t)byte;
+  for (int u = 0; u < U; ++u) {
+    const uint32_t t = (quad + u) * 4 + lane / 16;
+    slot[u] = t < (uint32_t)n_tokens ? slots[t] : -1;
+    if (slot[u] >= n_blocks * kTile) slot[u] = -1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
+    if (t < (uint32_t)n_tokens) load_elems<T, 8>((which ? v + t * ld_v : k + t * ld_k) + (size_t)h * kHeadDim + 8 * m, x[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[u][e]) & 0x7fffffffu);
+    top = max(top, xor_shfl_u32(top, 1));
+    top = max(top, xor_shfl_u32(top, 2));
+    const uint32_t byte = scale_byte(top);
+    const uint32_t codes = encode8(x[u], scale_of(byte));
+    if (slot[u] < 0) continue;
+    const size_t at = (size_t)(slot[u] / kTile) * H + h;
+    const int token = slot[u] % kTile;
+    *reinterpret_cast<uint32_t*>((which ? v_cache : k_cache) + at * kCodes4 + code_at(which, token, m)) = codes;
+    if (m % 4 == 0) scales[at * kScales4 + (which * kTile + token) * kGroups4 + m / 4] = (uint8_t)byte;
+  }
 }
 
 // ---------------------------------------------------------------- reading back
+
+constexpr size_t kL2Bytes = 32u << 20;  // of the eight dies
 
 struct Read4Args {
   const uint8_t *k, *v, *scales;
@@ -60,12 +75,20 @@ struct Read4Args {
 };
 
 // Output rows cu[b] .. cu[b + 1] - 1 are request b's tokens from starts[b] on.  A
-// work-group takes 16 rows: every wave finds their requests (64 offsets told
+// work-group takes 16 rows (float32: 8): every wave finds their requests (64 offsets told
 // apart at once, then the next 64 one after another) and slots, and the waves
-// share the heads' keys and values, four tokens of one head a load.
-constexpr int kReadRows = 16;
+// share the heads' keys and values, 16 bytes of output a lane.
+//
+// Bound by its stores: a wave's fill whole lines, and past what the L2s hold (NT)
+// they do not stay there: 470 MB in 98 us, 4.8 TB/s (137 with stores that stay, 176
+// with 32 bytes a lane); 310 MB as bf16 in 58 (78).
 template <typename T>
+constexpr int read_rows() {
+  return 4 * kWave / (kHeadDim * (int)sizeof(T) / 16);
+}
+template <typename T, bool NT>
 __global__ __launch_bounds__(256) void cache4_read_kernel(Read4Args a) {
+  constexpr int kReadRows = read_rows<T>();
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int t0 = blockIdx.x * kReadRows, t = t0 + lane % kReadRows;
   auto at = [&](int b) { return min(max(a.cu[b], 0), a.T); };
@@ -101,17 +124,18 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(Read4Args a) {
   }
   const uint64_t rows = __ballot(row);
   if (!rows) return;
-  const int m = lane % 16, q = lane / 16;
-  constexpr int kQuads = kReadRows / 4;
-  int blks[kQuads], tokens[kQuads];
+  // a lane stores 16 bytes: kDims elements of one row
+  constexpr int kDims = 16 / sizeof(T), kLanes = kHeadDim / kDims, kAtOnce = kWave / kLanes, kLoads = kReadRows / kAtOnce;
+  const int c = lane % kLanes, m = c * kDims / 8, q = lane / kLanes;
+  int blks[kLoads], tokens[kLoads];
 #pragma unroll
-  for (int u = 0; u < kQuads; ++u) blks[u] = __shfl(blk, 4 * u + q), tokens[u] = __shfl(token, 4 * u + q);
+  for (int u = 0; u < kLoads; ++u) blks[u] = __shfl(blk, kAtOnce * u + q), tokens[u] = __shfl(token, kAtOnce * u + q);
   const int from = a.k_out ? 0 : a.H, to = a.v_out ? 2 * a.H : a.H;
   for (int hw = from + blockIdx.y * 4 + wave; hw < to; hw += gridDim.y * 4) {
     const int which = hw >= a.H, h = which ? hw - a.H : hw;
-    uint32_t codes[kQuads], s[kQuads];
+    uint32_t codes[kLoads], s[kLoads];
 #pragma unroll
-    for (int u = 0; u < kQuads; ++u) {
+    for (int u = 0; u < kLoads; ++u) {
       codes[u] = 0, s[u] = 0;
       if (blks[u] >= 0) {
         const size_t x = (size_t)blks[u] + h;
@@ -120,20 +144,27 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(Read4Args a) {
       }
     }
 #pragma unroll
-    for (int u = 0; u < kQuads; ++u) {
-      const int i = 4 * u + q;
+    for (int u = 0; u < kLoads; ++u) {
+      const int i = kAtOnce * u + q;
       if (!(rows >> i & 1)) continue;
       T* out = (which ? (T*)a.v_out + (size_t)(t0 + i) * a.ld_v : (T*)a.k_out + (size_t)(t0 + i) * a.ld_k) +
-               (size_t)h * kHeadDim + 8 * m;
+               (size_t)h * kHeadDim + kDims * c;
+      uint32_t x[4];
       if constexpr (std::is_same_v<T, float>) {
-        float x[8];
-        decode8(codes[u], scale_of(s[u]), x);
-        store_elems<float, 8>(out, x);
+        const uint32_t four = codes[u] >> (c % 2 * 16);
+        const f32x2_t y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(four, scale_of(s[u]), 0);
+        const f32x2_t z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(four, scale_of(s[u]), 1);
+        x[0] = __float_as_uint(y[0]), x[1] = __float_as_uint(y[1]);
+        x[2] = __float_as_uint(z[0]), x[3] = __float_as_uint(z[1]);
       } else {
-        uint32_t x[4];
         decode8(codes[u], scale_of(s[u]), x);
-        *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
       }
+      typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+      const u32x4_t v = {x[0], x[1], x[2], x[3]};
+      if constexpr (NT)
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(out));
+      else
+        *reinterpret_cast<u32x4_t*>(out) = v;
     }
   }
 }
@@ -867,6 +898,21 @@ bool eight4_better(long long pairs, int max_blocks) {
   return pairs <= 256 && max_blocks > (pairs > 128 ? 16 : 8);
 }
 
+template <typename T>
+int launch_read4(const Read4Args& a, hipStream_t s) {
+  const int sides = a.k_out && a.v_out ? 2 : 1;
+  // some 2,000 work-groups while the heads allow it
+  const int blocks = (a.T + read_rows<T>() - 1) / read_rows<T>(), most = (sides * a.H + 3) / 4;
+  int split = 2048 / blocks;
+  split = split < 1 ? 1 : split > most ? most : split;
+  const dim3 grid(blocks, split);
+  if ((size_t)a.T * sides * a.H * kHeadDim * sizeof(T) >= kL2Bytes)
+    hipLaunchKernelGGL((cache4_read_kernel<T, true>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((cache4_read_kernel<T, false>), grid, dim3(256), 0, s, a);
+  return launched() ? SAKI_OK : SAKI_ERR_HIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -885,11 +931,11 @@ int saki_cache4_write(const void* k, const void* v, int dtype, int T, int H_kv, 
       overlap(v_cache, codes, scales, n_scales))
     return SAKI_ERR_ARG;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  // tokens a launch: its waves, one per four tokens of a head, in 2^23 work-groups at most
-  const int most = (int)((1LL << 25) / (2 * H_kv)) * 4;
+  // tokens a launch: its waves in 2^23 work-groups at most
+  const int most = (int)((1LL << 25) / (2 * H_kv)) * kWriteTokens;
   for (int t = 0; t < T; t += most) {
     const int n = T - t < most ? T - t : most;
-    const long long items = (long long)((n + 3) / 4) * 2 * H_kv;
+    const long long items = (long long)((n + kWriteTokens - 1) / kWriteTokens) * 2 * H_kv;
     const dim3 grid((unsigned)((items + 3) / 4));
     if (dtype == SAKI_F32)
       hipLaunchKernelGGL((cache4_write_kernel<float>), grid, dim3(256), 0, s, (const float*)k + t * ld_k,
@@ -918,16 +964,8 @@ int saki_cache4_read(const void* k_cache, const void* v_cache, const void* scale
     return SAKI_ERR_ARG;
   const Read4Args a{(const uint8_t*)k_cache, (const uint8_t*)v_cache, (const uint8_t*)scales, n_blocks, H_kv, tables,
                     max_blocks, starts, cu, B, T, k_out, v_out, ld_k, ld_v};
-  // some 2,000 work-groups while the heads allow it
-  const int blocks = (T + kReadRows - 1) / kReadRows, most = ((k_out && v_out ? 2 : 1) * H_kv + 3) / 4;
-  int split = 2048 / blocks;
-  split = split < 1 ? 1 : split > most ? most : split;
-  const dim3 grid(blocks, split);
-  if (dtype == SAKI_F32)
-    hipLaunchKernelGGL((cache4_read_kernel<float>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
-  else
-    hipLaunchKernelGGL((cache4_read_kernel<__bf16>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
-  return launched() ? SAKI_OK : SAKI_ERR_HIP;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return dtype == SAKI_F32 ? launch_read4<float>(a, s) : launch_read4<__bf16>(a, s);
 }
 
 size_t saki_cache4_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int max_blocks, int k) {

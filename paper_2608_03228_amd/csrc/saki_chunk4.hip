@@ -14,11 +14,11 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr float kScale = 0.08838834764831845f;  // 1 / sqrt(d)
-constexpr int kRows = 128;                      // query rows of a work-group (32 a wave)
+constexpr int kRows = 128;                      // query rows of a work-group (32 a wave), or half of them
 // A row's sums are scaled down only once a score passes the maximum they go by
 // by this many powers of two.
 constexpr float kSlack = 8.f;
-constexpr size_t kChunkPart = (size_t)kRows * (kHeadDim + 2);  // floats of a part: sums, maxima, weights
+constexpr size_t chunk_part(int rows) { return (size_t)rows * (kHeadDim + 2); }  // floats: sums, maxima, weights
 
 struct Chunk4Args {
   const void* q;
@@ -42,16 +42,25 @@ __device__ __forceinline__ float swap32(float v) { return xor_f32(v, 32); }
 // goes through the keys in the cache's blocks of 64: each thread holds 16 bytes of
 // the next block's keys and values, converts them to bf16 with their scales
 // (exactly) and puts them into LDS, two blocks deep, while the block before is
-// multiplied.  S^T = K Q^T leaves a lane with scores of one row, so the softmax is
+// multiplied.  Two groups a CU fill each other's pauses.  S^T = K Q^T leaves a lane with scores of one row, so the softmax is
 // in registers but for one exchange, and its weights are at once the operand of
 // O^T = V^T P^T, whose other operand the transposing LDS reads form.  bf16: weights
 // rounded to bf16; float32: queries and weights in three bf16 terms, 32 keys at a
 // time for the registers' sake.
-template <bool F32, bool SPLIT>
+//
+// Bound by power and the MFMA, with the softmax beside it: 2,000 tokens of 32 / 8
+// heads over 23,000 and 32,800 keys in 1,010-1,080 us, 0.86-0.92 PFLOP/s depending on
+// the card (a large bf16 matrix product reaches 1.27); float32, three products each,
+// 0.36 PFLOP/s.  256 rows a work-group, which halves the conversions, took as long.
+//
+// KS = 2: 64 rows, and two waves share a row's keys, 32 of each block; their sums
+// meet at the end (see chunk_plan).
+template <bool F32, bool SPLIT, int KS>
 __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, float* __restrict__ ws) {
   using T = std::conditional_t<F32, float, __bf16>;
   constexpr int kQT = F32 ? 3 : 1;
-  constexpr int NB = F32 ? 1 : 2;  // 32 keys each, between two looks at the maximum
+  constexpr int NB = F32 || KS == 2 ? 1 : 2;  // 32 keys each, between two looks at the maximum
+  constexpr int kBlockRows = kRows / KS;
   constexpr int kTileBytes = kTile * kHeadDim * 2;
   // two arrays, and the loop below unrolled over them: a read of one is then known
   // not to meet the writes to the other
@@ -59,10 +68,10 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int hk = blockIdx.x % a.H_kv, G = a.H_q / a.H_kv;
   const int part = blockIdx.x / a.H_kv, sp = SPLIT ? part % a.splits : 0, x = SPLIT ? part / a.splits : part;
-  const Block blk = saki_dev::find_block(a.cu, a.B, a.T, x, G, kRows);
+  const Block blk = saki_dev::find_block(a.cu, a.B, a.T, x, G, kBlockRows);
   if (blk.len == 0) return;
-  const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kRows);
-  const int n = lane % 32, h = lane / 32, rw = wave * 32;
+  const int n_rows = (int)min((long long)blk.len * G - blk.row0, (long long)kBlockRows);
+  const int n = lane % 32, h = lane / 32, rw = wave % (4 / KS) * 32;
 
   // this lane's row, its token, head and position; the least and largest position
   // of the group's rows and of the wave's
@@ -118,14 +127,21 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
       decode8(kc[s], scale_of(ks), w);
       *reinterpret_cast<uint4*>(to + r * 256 + (((tid % 4 * 4 + s) ^ (r % 16)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    float f[4];  // (the conversion reads the exponent alone)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) f[c] = __uint_as_float(__builtin_amdgcn_alignbit(ve[c], ve[c], turn));
+    if (t * kTile + kTile - 1 > pos_min) {
+      // a weight of zero has to make them zero: tokens that no row sees, and NaN where a row may not see it (below)
+      int u = t * kTile + v0;
+      asm volatile("" : "+v"(u));  // (what follows stays in the branch)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (u + c > pos_max || (u + c > pos_min && (__float_as_uint(f[c]) & 0x7f800000u) == 0x7f800000u)) f[c] = 0.f;
+    }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      float f = __uint_as_float(__builtin_amdgcn_alignbit(ve[c], ve[c], turn) & 0x7f800000u);
-      // a weight of zero has to make them zero: tokens that no row sees, and NaN where a row may not see it (below)
-      const int u = t * kTile + v0 + c;
-      if (u > pos_max || (u > pos_min && __float_as_uint(f) == 0x7f800000u)) f = 0.f;
       uint32_t w[4];
-      decode8(vc[c], f, w);
+      decode8(vc[c], f[c], w);
       *reinterpret_cast<uint4*>(to + kTileBytes + (v0 + c) * 256 + (((tid % 16) ^ (c * 4)) * 16)) =
           make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -145,7 +161,8 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
     if (rw >= n_rows || t * kTile > pos_hi) return;
     const uint8_t* vt = kt + kTileBytes;
 #pragma unroll
-    for (int b0 = 0; b0 < 2; b0 += NB) {
+    for (int half = 0; half < 2 / KS; half += NB) {
+      const int b0 = KS == 2 ? wave / 2 : half;
       f32x16_t s[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
@@ -172,7 +189,8 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
       top = fmaxf(top, swap32(top));
       if (__any(top > m + kSlack / (kScale * kLog2e))) {
         const float m1 = fmaxf(m, top);
-        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m1) * (kScale * kLog2e));
+        float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m1) * (kScale * kLog2e));
+        asm volatile("" : "+v"(keep));  // (the products below stay in the branch)
         m = m1;
         l *= keep;
 #pragma unroll
@@ -248,10 +266,36 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
   }
 
   l += swap32(l);
+  if constexpr (KS == 2) {  // the second waves' sums join the first ones', through the blocks' memory
+    __syncthreads();        // all blocks are read
+    float* y = (float*)(rw ? lds_b : lds_a);  // [64 sums][lane]
+    static_assert(2 * kTileBytes >= 64 * kWave * 4);
+    __shared__ float ml[2][2][kWave];
+    if (wave >= 2) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[(16 * d + i) * kWave + lane] = o[d][i];
+      ml[rw / 32][0][lane] = m;
+      ml[rw / 32][1][lane] = l;
+    }
+    __syncthreads();
+    if (wave >= 2) return;
+    const float m2 = ml[rw / 32][0][lane], l2 = ml[rw / 32][1][lane], m1 = fmaxf(m, m2);
+    const float ref = m1 == -INFINITY ? 0.f : m1;
+    const float e1 = __builtin_amdgcn_exp2f((m - ref) * (kScale * kLog2e));
+    const float e2 = __builtin_amdgcn_exp2f((m2 - ref) * (kScale * kLog2e));
+    m = m1;
+    l = l * e1 + l2 * e2;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * e1 + y[(16 * d + i) * kWave + lane] * e2;
+  }
   if (rw + n >= n_rows) return;
   if constexpr (SPLIT) {
-    float* w = ws + ((size_t)(x * a.H_kv + hk) * a.splits + sp) * kChunkPart;
-    if (h == 0) w[kRows * kHeadDim + rw + n] = m, w[kRows * (kHeadDim + 1) + rw + n] = l;
+    float* w = ws + ((size_t)(x * a.H_kv + hk) * a.splits + sp) * chunk_part(kBlockRows);
+    if (h == 0) w[kBlockRows * kHeadDim + rw + n] = m, w[kBlockRows * (kHeadDim + 1) + rw + n] = l;
     if (t0 >= t1) return;
     w += (rw + n) * kHeadDim + 4 * h;
 #pragma unroll
@@ -276,61 +320,134 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
   }
 }
 
-// Joins a row block's parts: 8 threads a row, 16 dims each.
-template <bool F32>
+// Joins a row's parts: a wave a row.  Lanes hold the parts' maxima and weights, 64 at
+// a time, then half of the wave sums every second part, 4 dims a lane, eight parts'
+// loads at once (a part after another, 51 parts of 100 tokens over 32,768 keys of
+// one head took 50 us).
+template <bool F32, int KS>
 __global__ __launch_bounds__(256) void cache4_gather_kernel(Chunk4Args a, const float* __restrict__ ws) {
   using T = std::conditional_t<F32, float, __bf16>;
+  constexpr int kBlockRows = kRows / KS;
+  constexpr size_t kPart = chunk_part(kBlockRows);
+  const int lane = threadIdx.x % kWave, half = lane / 32, d0 = lane % 32 * 4;
   const int hk = blockIdx.x % a.H_kv, x = blockIdx.x / a.H_kv, G = a.H_q / a.H_kv;
-  const Block blk = saki_dev::find_block(a.cu, a.B, a.T, x, G, kRows);
-  if (blk.len == 0) return;
-  const int i = blockIdx.y * 32 + threadIdx.x / 8, d0 = threadIdx.x % 8 * 16;
-  if (i >= (long long)blk.len * G - blk.row0) return;
-  const float* w = ws + (size_t)(x * a.H_kv + hk) * a.splits * kChunkPart;
-  float M = -INFINITY, L = 0.f, y[16];
-  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, w[s * kChunkPart + kRows * kHeadDim + i]);
+  const Block blk = saki_dev::find_block(a.cu, a.B, a.T, x, G, kBlockRows);
+  const int i = blockIdx.y * 4 + threadIdx.x / kWave;
+  if (blk.len == 0 || i >= (long long)blk.len * G - blk.row0) return;
+  const float* w = ws + (size_t)(x * a.H_kv + hk) * a.splits * kPart;
+  const float *wm = w + kBlockRows * kHeadDim + i, *wl = wm + kBlockRows;
+  float M = -INFINITY;
+  for (int s = lane; s < a.splits; s += kWave) M = fmaxf(M, wm[s * kPart]);
+#pragma unroll
+  for (int y = 1; y < kWave; y <<= 1) M = fmaxf(M, xor_f32(M, y));
   const float ref = M == -INFINITY ? 0.f : M;
+  float L = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.splits; s0 += kWave) {
+    const int n = min(a.splits - s0, kWave);
+    float e = 0.f;  // a part's factor; 0: no key of it is seen (a NaN goes on)
+    if (lane < n) {
+      const float l = wl[(s0 + lane) * kPart];
+      if (l != 0.f) e = __builtin_amdgcn_exp2f((wm[(s0 + lane) * kPart] - ref) * (kScale * kLog2e)), L += l * e;
+    }
+    constexpr int kAtOnce = 4;
+    for (int s = 0; s < n; s += 2 * kAtOnce) {
+      float4 z[kAtOnce];
+      float f[kAtOnce];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) y[e] = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float* p = w + s * kChunkPart;
-    const float l = p[kRows * (kHeadDim + 1) + i];
-    if (l == 0.f) continue;  // no key of the part is seen (a NaN goes on)
-    const float f = __builtin_amdgcn_exp2f((p[kRows * kHeadDim + i] - ref) * (kScale * kLog2e));
-    float z[16];
-    load_elems<float, 16>(p + (size_t)i * kHeadDim + d0, z);
-    L += l * f;
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int t = s + 2 * u + half;
+        f[u] = __shfl(e, t % kWave);
+        z[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (t < n && f[u] != 0.f) z[u] = *reinterpret_cast<const float4*>(w + (s0 + t) * kPart + i * kHeadDim + d0);
+      }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) y[e] += z[e] * f;
+      for (int u = 0; u < kAtOnce; ++u)
+        sum[0] += z[u].x * f[u], sum[1] += z[u].y * f[u], sum[2] += z[u].z * f[u], sum[3] += z[u].w * f[u];
+    }
   }
+#pragma unroll
+  for (int y = 1; y < kWave; y <<= 1) L += xor_f32(L, y);
   const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) y[e] *= inv;
+  for (int d = 0; d < 4; ++d) sum[d] = (sum[d] + xor_f32(sum[d], 32)) * inv;
   const int row = blk.row0 + i;
-  store_elems<T, 16>((T*)a.out + ((size_t)(blk.start + row / G) * a.H_q + hk * G + row % G) * kHeadDim + d0, y);
+  if (half == 0)
+    store_elems<T, 4>((T*)a.out + ((size_t)(blk.start + row / G) * a.H_q + hk * G + row % G) * kHeadDim + d0, sum);
 }
 
-// Row blocks of the packed tokens, at most.
-long long chunk_blocks(int T, int B, int G) { return (long long)T * G / kRows + B; }
+// How a call is divided.
+struct ChunkPlan {
+  bool halves;       // 64 rows a work-group
+  long long groups;  // row blocks of the packed tokens (at most) times KV heads
+  int splits;        // work-groups that share a block's keys
+  size_t ws_bytes() const {
+    return splits > 1 ? (size_t)groups * splits * chunk_part(halves ? kRows / 2 : kRows) * sizeof(float) : 256;
+  }
+};
 
-// Work-groups that share a row block's keys: as many as fill the GPU, two a CU,
-// with at least four cache blocks each.
-int chunk_splits(long long groups, int max_blocks) {
-  long long s = 512 / groups;
-  const long long most = max_blocks / 4;
-  s = s > most ? most : s;
-  return (int)(s < 1 ? 1 : s);
+// Row blocks that hold rows, more or less: a request has one at least, its last one half full.
+long long blocks_of(long long rows, int block_rows, int B) {
+  const long long n = rows / block_rows + (B + 1) / 2;
+  return n > B ? n : B;
+}
+
+// Which blocks and how many shares take the least time, by what one cache block
+// takes a work-group: us, alone on a CU and beside another (256 and 512 groups
+// over 16,384 tokens and more),
+//              bf16           float32
+//   128 rows   1.44 / 2.31    3.15 / 5.44
+//    64 rows   1.06 / 1.47    1.74 / 2.96
+// and the join: 4 us, and a part written and read.  The tables' width stands for
+// the lengths, which are on the device.
+ChunkPlan chunk_plan(int dtype, int T, int B, int G, int H_kv, int max_blocks) {
+  static const float kTake[2][2][2] = {{{3.15f, 5.44f}, {1.74f, 2.96f}}, {{1.44f, 2.31f}, {1.06f, 1.47f}}};
+  const long long rows = (long long)T * G;
+  ChunkPlan best{false, 0, 0};
+  float least = 0.f;
+  for (int halves = 0; halves < 2; ++halves) {
+    const int block_rows = halves ? kRows / 2 : kRows;
+    const float* take = kTake[dtype == SAKI_BF16][halves];
+    const long long n = blocks_of(rows, block_rows, B) * H_kv;
+    const long long shares[4] = {1, 256 / n, 512 / n, 1024 / n};
+    for (int i = 0; i < 4; ++i) {
+      const long long most = max_blocks < 4 ? 1 : max_blocks / 2, s = shares[i] < most ? shares[i] : most;  // two blocks each at least
+      if (i && s <= 1) continue;
+      const long long all = n * s, rest = all % 512;
+      const float each = (float)((max_blocks + s - 1) / s);
+      float us = each * ((float)(all / 512) * take[1] + (rest == 0 ? 0.f : take[rest > 256]));
+      if (s > 1) us += 4.f + (float)all * (float)block_rows * 2.1e-4f;
+      if (best.groups == 0 || us < least) {
+        least = us;
+        best = ChunkPlan{halves == 1, (rows / block_rows + B) * H_kv, (int)s};
+      }
+    }
+  }
+  return best;
+}
+
+template <bool F32, int KS>
+int launch_chunk(const ChunkPlan& p, const Chunk4Args& a, void* ws, hipStream_t s) {
+  const dim3 grid((unsigned)(p.groups * p.splits));
+  if (p.splits == 1) {
+    hipLaunchKernelGGL((cache4_prompt_kernel<F32, false, KS>), grid, dim3(256), 0, s, a, nullptr);
+    return launched() ? SAKI_OK : SAKI_ERR_HIP;
+  }
+  hipLaunchKernelGGL((cache4_prompt_kernel<F32, true, KS>), grid, dim3(256), 0, s, a, (float*)ws);
+  if (!launched()) return SAKI_ERR_HIP;
+  hipLaunchKernelGGL((cache4_gather_kernel<F32, KS>), dim3((unsigned)p.groups, kRows / KS / 4), dim3(256), 0, s, a,
+                     (const float*)ws);
+  return launched() ? SAKI_OK : SAKI_ERR_HIP;
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t saki_cache4_prompt_workspace_bytes(int T, int B, int H_q, int H_kv, int max_blocks) {
-  if (T < 0 || B < 0 || H_q <= 0 || H_kv <= 0 || H_q % H_kv != 0 || max_blocks <= 0) return 0;
+size_t saki_cache4_prompt_workspace_bytes(int dtype, int T, int B, int H_q, int H_kv, int max_blocks) {
+  if (T < 0 || B < 0 || H_q <= 0 || H_kv <= 0 || H_q % H_kv != 0 || max_blocks <= 0 || !type_ok(dtype))
+    return 0;
   if (T == 0 || B == 0) return 256;
-  const long long groups = chunk_blocks(T, B, H_q / H_kv) * H_kv;
-  const int splits = chunk_splits(groups, max_blocks);
-  return splits > 1 ? (size_t)groups * splits * kChunkPart * sizeof(float) : 256;
+  return chunk_plan(dtype, T, B, H_q / H_kv, H_kv, max_blocks).ws_bytes();
 }
 
 int saki_cache4_prompt(const void* q, int dtype, int T, int B, int H_q, int H_kv, int d, size_t ld_q,
@@ -341,36 +458,18 @@ int saki_cache4_prompt(const void* q, int dtype, int T, int B, int H_q, int H_kv
   const int st = check_cache4(k_cache, v_cache, scales, n_blocks, H_kv);
   if (st != SAKI_OK) return st;
   const int G = H_q / H_kv;
-  const long long groups = chunk_blocks(T, B, G) * H_kv;
-  if (d != kHeadDim || !type_ok(dtype) || T > kMaxTokens || max_blocks > INT_MAX / kTile - 1 ||
-      (long long)T * G >= INT_MAX || groups > (1 << 23) || H_q > 65535)
+  if (d != kHeadDim || !type_ok(dtype) || T > kMaxTokens || B > INT_MAX / 2 || max_blocks > INT_MAX / kTile - 1 ||
+      (long long)T * G >= INT_MAX / 2 || 2 * ((long long)T * G / kRows + B) * H_kv > (1 << 23) || H_q > 65535)
     return SAKI_ERR_UNSUPPORTED;
   if (T == 0 || B == 0) return SAKI_OK;
   if (!out || !aligned(out, 16) || !tables || !lens || !cu || !rows_ok(q, ld_q, H_q, dtype)) return SAKI_ERR_ARG;
-  const int splits = chunk_splits(groups, max_blocks);
-  if (splits > 1 && (!ws || !aligned(ws, 16) || ws_bytes < saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks)))
-    return SAKI_ERR_WORKSPACE;
+  const ChunkPlan p = chunk_plan(dtype, T, B, G, H_kv, max_blocks);
+  if (p.splits > 1 && (!ws || !aligned(ws, 16) || ws_bytes < p.ws_bytes())) return SAKI_ERR_WORKSPACE;
   const Chunk4Args a{q, ld_q, (const uint8_t*)k_cache, (const uint8_t*)v_cache, (const uint8_t*)scales, n_blocks,
-                     tables, max_blocks, lens, cu, B, H_q, H_kv, T, out, splits};
+                     tables, max_blocks, lens, cu, B, H_q, H_kv, T, out, p.splits};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const dim3 grid((unsigned)(groups * splits)), join((unsigned)groups, kRows / 32);
-  if (splits == 1) {
-    if (dtype == SAKI_F32)
-      hipLaunchKernelGGL((cache4_prompt_kernel<true, false>), grid, dim3(256), 0, s, a, nullptr);
-    else
-      hipLaunchKernelGGL((cache4_prompt_kernel<false, false>), grid, dim3(256), 0, s, a, nullptr);
-    return launched() ? SAKI_OK : SAKI_ERR_HIP;
-  }
-  if (dtype == SAKI_F32) {
-    hipLaunchKernelGGL((cache4_prompt_kernel<true, true>), grid, dim3(256), 0, s, a, (float*)ws);
-    if (!launched()) return SAKI_ERR_HIP;
-    hipLaunchKernelGGL((cache4_gather_kernel<true>), join, dim3(256), 0, s, a, (const float*)ws);
-  } else {
-    hipLaunchKernelGGL((cache4_prompt_kernel<false, true>), grid, dim3(256), 0, s, a, (float*)ws);
-    if (!launched()) return SAKI_ERR_HIP;
-    hipLaunchKernelGGL((cache4_gather_kernel<false>), join, dim3(256), 0, s, a, (const float*)ws);
-  }
-  return launched() ? SAKI_OK : SAKI_ERR_HIP;
+  if (dtype == SAKI_F32) return p.halves ? launch_chunk<true, 2>(p, a, ws, s) : launch_chunk<true, 1>(p, a, ws, s);
+  return p.halves ? launch_chunk<false, 2>(p, a, ws, s) : launch_chunk<false, 1>(p, a, ws, s);
 }
 
 }  // extern "C"

@@ -81,7 +81,7 @@ def lib():
         "saki_cache4_attend_workspace_bytes": (sz, [ip, ip, ip, ip, ip, ip]),
         "saki_cache4_attend": (ip, [vp, ip, ip, ip, ip, ip, ip, vp, vp, vp, ip, vp, ip, vp, vp, ip,
                                     vp, vp, sz, vp]),
-        "saki_cache4_prompt_workspace_bytes": (sz, [ip, ip, ip, ip, ip]),
+        "saki_cache4_prompt_workspace_bytes": (sz, [ip, ip, ip, ip, ip, ip]),
         "saki_cache4_prompt": (ip, [vp, ip, ip, ip, ip, ip, ip, sz, vp, vp, vp, ip, vp, ip, vp, vp,
                                     vp, vp, sz, vp]),
     }
@@ -815,8 +815,9 @@ def saki_cache4_attend(q, k_cache, v_cache, scales, tables, lens, top_idx=None, 
                           tables, lens, top_idx, out, ws, stream)
 
 
-def saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks) -> int:
-    return int(lib().saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks))
+def saki_cache4_prompt_workspace_bytes(dtype: str, T, B, H_q, H_kv, max_blocks) -> int:
+    return int(lib().saki_cache4_prompt_workspace_bytes(_DTYPES[dtype], T, B, H_q, H_kv,
+                                                        max_blocks))
 
 
 def saki_cache4_prompt(q, k_cache, v_cache, scales, tables, lens, cu, out=None, ws=None,
@@ -843,7 +844,7 @@ def saki_cache4_prompt(q, k_cache, v_cache, scales, tables, lens, cu, out=None, 
         out = _new(stream, shape, dt, q.device)
     wp, wn = None, 0
     if ws is None:
-        need = _args_mod.saki_cache4_prompt_workspace_bytes(T, B, H_q, H_kv, max_blocks)
+        need = _args_mod.saki_cache4_prompt_workspace_bytes(code, T, B, H_q, H_kv, max_blocks)
         if need > NO_WORKSPACE:
             ws = _new(stream, need, torch.uint8, q.device, result=False)
     if ws is not None:

@@ -92,7 +92,7 @@ PROMPT = ("q dtype T B H_q H_kv d ld_q k_cache v_cache scales n_blocks tables ma
     (dict(scales=ODD), ARG), (dict(ws=None), WS), (dict(ws=ODD), WS), (dict(ws_bytes=100), WS),
 ])
 def test_prompt(lib, kw, status):
-    need = lib.saki_cache4_prompt_workspace_bytes(5, 2, 4, 2, 100)
+    need = lib.saki_cache4_prompt_workspace_bytes(1, 5, 2, 4, 2, 100)
     assert need > 256
     good = [P, 1, 5, 2, 4, 2, 128, 512, K, V, SC, 9, P, 100, P, P, P, P, need, None]
     assert change(lib.saki_cache4_prompt, good, PROMPT, **kw) == status
@@ -102,11 +102,12 @@ def test_workspace_sizes(lib):
     assert lib.saki_cache4_attend_workspace_bytes(1, 4, 3, 1, 100, 0) == 0
     assert lib.saki_cache4_attend_workspace_bytes(1, 4, 2, 1, 100, 64) == 256
     assert 256 < lib.saki_cache4_attend_workspace_bytes(64, 32, 8, 1, 1 << 20, 0) <= 32 << 20
-    assert lib.saki_cache4_prompt_workspace_bytes(5, 2, 4, 3, 100) == 0
-    assert lib.saki_cache4_prompt_workspace_bytes(0, 2, 4, 2, 100) == 256
-    assert lib.saki_cache4_prompt_workspace_bytes(1 << 20, 2, 4, 2, 100) == 256
+    assert lib.saki_cache4_prompt_workspace_bytes(1, 5, 2, 4, 3, 100) == 0
+    assert lib.saki_cache4_prompt_workspace_bytes(2, 5, 2, 4, 2, 100) == 0
+    assert lib.saki_cache4_prompt_workspace_bytes(1, 0, 2, 4, 2, 100) == 256
+    assert lib.saki_cache4_prompt_workspace_bytes(0, 1 << 20, 2, 4, 2, 100) == 256
     # bounded, whatever the table's width
-    assert lib.saki_cache4_prompt_workspace_bytes(1, 1, 32, 8, 1 << 24) <= 128 << 20
+    assert lib.saki_cache4_prompt_workspace_bytes(1, 1, 1, 32, 8, 1 << 24) <= 128 << 20
 
 
 @pytest.mark.parametrize("call", [
