@@ -162,6 +162,23 @@ def test_read(cu, starts, H, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_read_of_more_than_the_caches_hold(dt):
+    rng = np.random.default_rng(5)
+    H, blocks = 4, 600
+    cache = random_cache(blocks, H, rng)
+    tab = rng.permutation(blocks).reshape(3, 200)
+    cu, starts = np.array([0, 12800, 12800, 12800 + 12000]), [0, 5, 777]
+    k, v = torch.zeros((2, cu[-1] + 3, H, 128), device=DEV, dtype=DT[dt])
+    assert 2 * k.numel() * k.element_size() >= 32 << 20
+    S.saki_cache4_read(*on_gpu(cache), ints(tab), ints(cu), k, v, starts=ints(starts))
+    for got, x in zip((k, v), values(cache)):
+        want = np.zeros(got.shape)
+        want[:12800] = x[tab[0]].transpose(0, 2, 1, 3).reshape(-1, H, 128)
+        want[12800:24800] = x[tab[2]].transpose(0, 2, 1, 3).reshape(-1, H, 128)[777:12777]
+        np.testing.assert_array_equal(host(got), want)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_read_of_one_side_and_into_a_wider_row(dt):
     rng = np.random.default_rng(1)
     H, T = 2, 100
@@ -254,7 +271,7 @@ def test_attend(rows, lens, H_q, H_kv, Q, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [15, 70])
+@pytest.mark.parametrize("rows", [15, 70, 130])
 def test_attend_many_requests(rows, dt):
     rng = np.random.default_rng(0)
     lens = rng.integers(0, 70, 530).tolist()
@@ -270,6 +287,52 @@ def test_attend_table_entries_out_of_range():
     check_attend((q, cache, tab[:, :2].copy()), [1 << 30, 2147483647, 128], "f32")
     idx = np.tile(np.array([0, 200, 450, 2147483647, 499, -3]), (3, 4, 1, 1))
     check_attend((q, cache, tab), lens, "f32", top_idx=idx)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H_q,H_kv,Q", [
+    ([1200, 700, 64], 8, 8, 1), ([500] * 20, 8, 4, 2), ([1100, 3] * 70, 4, 2, 1), ([9000], 3, 1, 1), ([20000, 5], 4, 2, 4),
+])
+def test_attend_more_shapes(lens, H_q, H_kv, Q, dt):
+    """Eight waves to a pair and four, one head's keys in many parts, many pairs joined."""
+    check_attend(attend_case(lens, H_q, H_kv, Q, dt), lens, dt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [None, 70])
+@pytest.mark.parametrize("H_q", [3, 8, 13])   # of one KV head: four, two and one term side by side
+def test_attend_queries_that_are_not_finite(H_q, rows, dt):
+    """Such a query's row is NaN and the others are what they were."""
+    case = attend_case([300, 70], H_q, 1, 1, dt, rows)
+    q, cache, tab = case
+    clean = host(S.saki_cache4_attend(dev(q, DT[dt]), *on_gpu(cache), ints(tab), ints([300, 70])))
+    q = q.copy()
+    q[0, 1, 0, 7], q[1, 0, 0, 100], q[1, 2, 0, 31] = np.nan, np.inf, -np.inf
+    got = host(S.saki_cache4_attend(dev(q, DT[dt]), *on_gpu(cache), ints(tab), ints([300, 70])))
+    for b, h in ((0, 1), (1, 0), (1, 2)):
+        assert np.isnan(got[b, h]).all()
+        got[b, h] = clean[b, h]
+    np.testing.assert_array_equal(got, clean)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("how", ["all", "lists", "chunk"])
+def test_attention_over_scales_far_apart(how, dt):
+    """Values of 2^90 in one head and 2^-90 in the other, groups of a token 2^30 apart,
+    and keys of 2^-90 under queries of 2^88."""
+    lens = [150, 40]
+    q, cache, tab = attend_case(lens, 4, 2, 1, dt, stale=False)
+    rng = np.random.default_rng(1)
+    cache[2][:, 0, 1] = 127 + 90 - rng.choice([0, 30], cache[2][:, 0, 1].shape)
+    cache[2][:, 1, 1] = 127 - 60 - rng.choice([0, 30], cache[2][:, 1, 1].shape)
+    cache[2][:, 1, 0] = 127 - 90
+    q[:, 2:] *= 2.0 ** 88
+    q = rounded(q, dt)
+    idx = np.stack([rng.integers(0, n, (4, 1, 33)) for n in lens]) if how == "lists" else None
+    if how != "chunk":
+        check_attend((q, cache, tab), lens, dt, top_idx=idx)
+    else:
+        check_chunk((q[:, :, 0], cache, tab, lens, np.array([0, 1, 2])), dt)
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
@@ -357,6 +420,38 @@ def test_prompt_tokens_of_no_request_and_missing_blocks(rows, dt):
     assert (want[:10] == 0).all() and (want[120:] == 0).all()
     # past the table's room
     check_chunk((q, cache, tab[:, :2].copy(), [1000, 170, 9], cu), dt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ctx,new,H_q,H_kv", [
+    ([100] * 4, [4000, 3999, 4001, 3500], 4, 1), ([0], [2100], 8, 8), ([1000, 30], [700, 650], 32, 8),
+])
+def test_prompt_of_many_rows(ctx, new, H_q, H_kv, dt):
+    """Whole blocks of 128 rows, shared and not; every 89th token and the requests' ends against the oracle."""
+    q, cache, tab, lens, cu = chunk_case(ctx, new, H_q, H_kv, dt)
+    got = host(S.saki_cache4_prompt(dev(q, DT[dt]), *on_gpu(cache), ints(tab), ints(lens), ints(cu)))
+    assert np.isfinite(got).all()
+    k, v = values(cache)
+    for b, n in enumerate(new):
+        for i in sorted({*range(b, n, 89), 0, 31, 32, 127, 128, n - 1}):
+            t = cu[b] + i
+            want, mass, size = O.cache4_prompt(q[t:t + 1], k, v, tab[b:b + 1], [lens[b] - n + i + 1], [0, 1])
+            close(got[t:t + 1], want, attention_bound(want, mass, size, lens[b], dt, 2.0 ** -8))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [None, 400])
+def test_prompt_queries_that_are_not_finite(rows, dt):
+    q, cache, tab, lens, cu = chunk_case([200], [50], 4, 2, dt, rows)
+    args = *on_gpu(cache), ints(tab), ints(lens), ints(cu)
+    clean = host(S.saki_cache4_prompt(dev(q, DT[dt]), *args))
+    q = q.copy()
+    q[3, 1, 7], q[20, 0, 100], q[49, 3, 64] = np.nan, np.inf, -np.inf
+    got = host(S.saki_cache4_prompt(dev(q, DT[dt]), *args))
+    for t, h in ((3, 1), (20, 0), (49, 3)):
+        assert np.isnan(got[t, h]).all()
+        got[t, h] = clean[t, h]
+    np.testing.assert_array_equal(got, clean)
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
