@@ -67,6 +67,10 @@ __device__ __forceinline__ void decode8(uint32_t c, float s, float* x) {
   x[4] = d[0], x[5] = d[1], x[6] = e[0], x[7] = e[1];
 }
 
+// Tables are read by scalar loads: a wait for a vector load would wait for the tiles that are on their way
+// too.
+typedef __attribute__((address_space(4))) int const_int;
+
 // Where 8 dims (8 m ..) of a block's token lie: bytes from the block's codes.
 __device__ __forceinline__ int code_at(int which, int token, int m) {
   return which ? token / 4 * 256 + m * 16 + token % 4 * 4 : token * (kHeadDim / 2) + m * 4;

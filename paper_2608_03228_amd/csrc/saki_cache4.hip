@@ -180,9 +180,6 @@ __device__ __forceinline__ long long uniform(long long x) {
   return (long long)((uint64_t)hi << 32 | lo);
 }
 
-// Tables are read by scalar loads: a wait for a vector load would wait for the tiles that are on their way too.
-typedef __attribute__((address_space(4))) int const_int;
-
 constexpr int kTile4 = 2 * kCodes4 + kScales4;  // bytes of a tile: keys, values, scales
 constexpr int kAttendGroups4 = 512;             // two a CU
 

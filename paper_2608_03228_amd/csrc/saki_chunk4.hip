@@ -49,9 +49,9 @@ __device__ __forceinline__ float swap32(float v) { return xor_f32(v, 32); }
 // time for the registers' sake.
 //
 // Bound by power and the MFMA, with the softmax beside it: 2,000 tokens of 32 / 8
-// heads over 23,000 and 32,800 keys in 1,010-1,080 us, 0.86-0.92 PFLOP/s depending on
-// the card (a large bf16 matrix product reaches 1.27); float32, three products each,
-// 0.36 PFLOP/s.  256 rows a work-group, which halves the conversions, took as long.
+// heads over 23,000 and 32,800 keys in 950-1,060 us, 0.88-0.98 PFLOP/s depending on
+// the card (a large bf16 matrix product reaches 1.17-1.27), the MFMA 41% busy;
+// float32, three products each, 0.36 PFLOP/s.  256 rows a work-group, which halves the conversions, took as long.
 //
 // KS = 2: 64 rows, and two waves share a row's keys, 32 of each block; their sums
 // meet at the end (see chunk_plan).
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
     }
   }
 
-  const int* table = a.tables + (size_t)blk.b * a.max_blocks;
+  const const_int* table = (const const_int*)(uintptr_t)(a.tables + (size_t)blk.b * a.max_blocks);
   auto block_of = [&](int t) __attribute__((always_inline)) {
     const int at = t < t1 ? table[t] : -1;
     return at < a.n_blocks ? at : -1;  // (below 0: none)
@@ -230,18 +230,22 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
     }
   };
 
-  int at0 = block_of(t0), at1 = block_of(t0 + 1);
+  int at0 = block_of(t0), at1 = block_of(t0 + 1), at2 = block_of(t0 + 2);
   fetch(at0);
   if (at0 >= 0) put(t0, lds_a);
+  // the queries are there: waited for in the loop, they would have it wait for the next block too (with tables
+  // read by vector loads, 1.05 us for 0.88 a block of 64 rows)
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
   fetch(at1);
   auto step = [&](int t, const uint8_t* now, uint8_t* next) __attribute__((always_inline)) {
     __syncthreads();  // block t is in `now`, and `next` is read
-    const int at2 = block_of(t + 2);
+    const int at3 = block_of(t + 3);
     if (at1 >= 0) put(t + 1, next);
     fetch(at2);
     if (at0 >= 0) tile(t, now);
     at0 = at1;
     at1 = at2;
+    at2 = at3;
   };
   for (int t = t0; t < t1; t += 2) {
     step(t, lds_a, lds_b);
@@ -395,12 +399,12 @@ long long blocks_of(long long rows, int block_rows, int B) {
 // takes a work-group: us, alone on a CU and beside another (256 and 512 groups
 // over 16,384 tokens and more),
 //              bf16           float32
-//   128 rows   1.44 / 2.31    3.15 / 5.44
-//    64 rows   1.06 / 1.47    1.74 / 2.96
+//   128 rows   1.28 / 2.04    2.88 / 4.85
+//    64 rows   0.88 / 1.31    1.65 / 2.65
 // and the join: 4 us, and a part written and read.  The tables' width stands for
 // the lengths, which are on the device.
 ChunkPlan chunk_plan(int dtype, int T, int B, int G, int H_kv, int max_blocks) {
-  static const float kTake[2][2][2] = {{{3.15f, 5.44f}, {1.74f, 2.96f}}, {{1.44f, 2.31f}, {1.06f, 1.47f}}};
+  static const float kTake[2][2][2] = {{{2.88f, 4.85f}, {1.65f, 2.65f}}, {{1.28f, 2.04f}, {0.88f, 1.31f}}};
   const long long rows = (long long)T * G;
   ChunkPlan best{false, 0, 0};
   float least = 0.f;
