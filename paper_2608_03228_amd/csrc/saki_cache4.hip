@@ -75,9 +75,10 @@ struct Read4Args {
 };
 
 // Output rows cu[b] .. cu[b + 1] - 1 are request b's tokens from starts[b] on.  A
-// work-group takes 16 rows (float32: 8): every wave finds their requests (64 offsets told
-// apart at once, then the next 64 one after another) and slots, and the waves
-// share the heads' keys and values, 16 bytes of output a lane.
+// work-group takes 16 rows (float32: 8): every wave finds their requests (of up to
+// 64 in its lanes; of more 64 told apart at once, then the next 64 one after
+// another) and slots, and the waves share the heads' keys and values, 16 bytes of
+// output a lane.
 //
 // Bound by its stores: a wave's fill whole lines, and past what the L2s hold (NT)
 // they do not stay there: 470 MB in 98 us, 4.8 TB/s (137 with stores that stay, 176
@@ -92,31 +93,45 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(Read4Args a) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int t0 = blockIdx.x * kReadRows, t = t0 + lane % kReadRows;
   auto at = [&](int b) { return min(max(a.cu[b], 0), a.T); };
-  int b = 0, n = a.B;  // the last request that starts at or before t0 is one of b .. b + n - 1
-  while (n > 1) {
-    const int step = (n + kWave - 1) / kWave, i = lane * step;
-    const uint64_t which = __ballot(i < n && at(b + i) <= t0);
-    const int part = which ? (63 - __builtin_clzll(which)) * step : 0;
-    n = min(n - part, step);
-    b += part;
-  }
-  const int first = at(0);
-  int mine = b;
-  for (int more = b + 1; more < a.B; more += kWave) {  // requests that start within the rows
-    const int c = more + lane < a.B ? at(more + lane) : a.T;
-    int j = 0;
-    for (; j < kWave; ++j) {
-      const int s = __builtin_amdgcn_readlane(c, j);
-      if (s >= t0 + kReadRows || more + j >= a.B) break;
-      if (s <= t) mine = more + j;
+  int mine = 0, first, begin, end, start;  // this row's request: its first row and the one behind its last, its first token
+  if (a.B <= kWave) {  // all offsets and starts in a wave's lanes, one read deep
+    const int c = at(min(lane, a.B)), last = at(a.B), s = a.starts && lane < a.B ? a.starts[lane] : 0;
+#pragma unroll
+    for (int half = kWave / 2; half; half >>= 1) {
+      const int x = __shfl(c, (mine + half) % kWave);
+      if (mine + half < a.B && x <= t) mine += half;
     }
-    if (j < kWave) break;
+    first = __shfl(c, 0);
+    begin = __shfl(c, mine), start = __shfl(s, mine);
+    end = __shfl(c, (mine + 1) % kWave);
+    if (mine + 1 == a.B) end = last;
+  } else {
+    int b = 0, n = a.B;  // the last request that starts at or before t0 is one of b .. b + n - 1
+    while (n > 1) {
+      const int step = (n + kWave - 1) / kWave, i = lane * step;
+      const uint64_t which = __ballot(i < n && at(b + i) <= t0);
+      const int part = which ? (63 - __builtin_clzll(which)) * step : 0;
+      n = min(n - part, step);
+      b += part;
+    }
+    mine = b;
+    for (int more = b + 1; more < a.B; more += kWave) {  // requests that start within the rows
+      const int c = more + lane < a.B ? at(more + lane) : a.T;
+      int j = 0;
+      for (; j < kWave; ++j) {
+        const int s = __builtin_amdgcn_readlane(c, j);
+        if (s >= t0 + kReadRows || more + j >= a.B) break;
+        if (s <= t) mine = more + j;
+      }
+      if (j < kWave) break;
+    }
+    first = at(0), begin = at(mine), end = at(mine + 1), start = a.starts ? a.starts[mine] : 0;
   }
   // (block * H) and token, or where there is no such token: its row is zero
   int blk = -1, token = 0;
-  const bool row = t >= first && t < a.T && t < at(mine + 1);
+  const bool row = t >= first && t < a.T && t < end;
   if (row) {
-    const long long p = (long long)(a.starts ? a.starts[mine] : 0) + (t - at(mine));
+    const long long p = (long long)start + (t - begin);
     if (p >= 0 && p / kTile < a.max_blocks) {
       const int x = a.tables[(size_t)mine * a.max_blocks + p / kTile];
       if (x >= 0 && x < a.n_blocks) blk = x * a.H, token = (int)(p % kTile);

@@ -324,59 +324,69 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
   }
 }
 
-// Joins a row's parts: a wave a row.  Lanes hold the parts' maxima and weights, 64 at
-// a time, then half of the wave sums every second part, 4 dims a lane, eight parts'
-// loads at once (a part after another, 51 parts of 100 tokens over 32,768 keys of
-// one head took 50 us).
-template <bool F32, int KS>
+// Joins a row's parts.  LANES = 64: a wave a row; its lanes hold the parts' maxima
+// and weights, 64 at a time, then half of the wave sums every second part, 4 dims a
+// lane, eight parts' loads at once (a part after another, 51 parts of 100 tokens
+// over 32,768 keys of one head took 50 us).  LANES = 16, for up to 6 parts: four rows
+// a wave, 8 dims a lane (two parts of 28,672 float32 rows: 5.5 us less).
+template <bool F32, int KS, int LANES>
 __global__ __launch_bounds__(256) void cache4_gather_kernel(Chunk4Args a, const float* __restrict__ ws) {
   using T = std::conditional_t<F32, float, __bf16>;
-  constexpr int kBlockRows = kRows / KS;
+  constexpr int kBlockRows = kRows / KS, kAtOnce = 4;
+  constexpr int kDims = LANES == 64 ? 4 : 8, kSide = LANES * kDims / kHeadDim;  // parts side by side
   constexpr size_t kPart = chunk_part(kBlockRows);
-  const int lane = threadIdx.x % kWave, half = lane / 32, d0 = lane % 32 * 4;
+  const int c = threadIdx.x % LANES, side = c / (kHeadDim / kDims), d0 = c % (kHeadDim / kDims) * kDims;
+  const int first = threadIdx.x % kWave - c;  // the row's lanes
   const int hk = blockIdx.x % a.H_kv, x = blockIdx.x / a.H_kv, G = a.H_q / a.H_kv;
   const Block blk = saki_dev::find_block(a.cu, a.B, a.T, x, G, kBlockRows);
-  const int i = blockIdx.y * 4 + threadIdx.x / kWave;
-  if (blk.len == 0 || i >= (long long)blk.len * G - blk.row0) return;
+  const int i = blockIdx.y * (256 / LANES) + threadIdx.x / LANES;
+  const bool in = i < (long long)blk.len * G - blk.row0;
+  if (blk.len == 0 || !__any(in)) return;
   const float* w = ws + (size_t)(x * a.H_kv + hk) * a.splits * kPart;
   const float *wm = w + kBlockRows * kHeadDim + i, *wl = wm + kBlockRows;
+  const int parts = in ? a.splits : 0;
   float M = -INFINITY;
-  for (int s = lane; s < a.splits; s += kWave) M = fmaxf(M, wm[s * kPart]);
+  for (int s = c; s < parts; s += LANES) M = fmaxf(M, wm[s * kPart]);
 #pragma unroll
-  for (int y = 1; y < kWave; y <<= 1) M = fmaxf(M, xor_f32(M, y));
+  for (int y = 1; y < LANES; y <<= 1) M = fmaxf(M, xor_f32(M, y));
   const float ref = M == -INFINITY ? 0.f : M;
-  float L = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.splits; s0 += kWave) {
-    const int n = min(a.splits - s0, kWave);
+  float L = 0.f, sum[kDims];
+#pragma unroll
+  for (int d = 0; d < kDims; ++d) sum[d] = 0.f;
+  for (int s0 = 0; s0 < a.splits; s0 += LANES) {
+    const int n = min(a.splits - s0, LANES);
     float e = 0.f;  // a part's factor; 0: no key of it is seen (a NaN goes on)
-    if (lane < n) {
-      const float l = wl[(s0 + lane) * kPart];
-      if (l != 0.f) e = __builtin_amdgcn_exp2f((wm[(s0 + lane) * kPart] - ref) * (kScale * kLog2e)), L += l * e;
+    if (s0 + c < parts) {
+      const float l = wl[(s0 + c) * kPart];
+      if (l != 0.f) e = __builtin_amdgcn_exp2f((wm[(s0 + c) * kPart] - ref) * (kScale * kLog2e)), L += l * e;
     }
-    constexpr int kAtOnce = 4;
-    for (int s = 0; s < n; s += 2 * kAtOnce) {
-      float4 z[kAtOnce];
-      float f[kAtOnce];
+    for (int s = 0; s < n; s += kSide * kAtOnce) {
+      float z[kAtOnce][kDims], f[kAtOnce];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int t = s + 2 * u + half;
-        f[u] = __shfl(e, t % kWave);
-        z[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (t < n && f[u] != 0.f) z[u] = *reinterpret_cast<const float4*>(w + (s0 + t) * kPart + i * kHeadDim + d0);
+        const int t = s + kSide * u + side;
+        f[u] = __shfl(e, first + t % LANES);
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) z[u][d] = 0.f;
+        if (t < n && f[u] != 0.f) load_elems<float, kDims>(w + (s0 + t) * kPart + i * kHeadDim + d0, z[u]);
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u)
-        sum[0] += z[u].x * f[u], sum[1] += z[u].y * f[u], sum[2] += z[u].z * f[u], sum[3] += z[u].w * f[u];
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) sum[d] += z[u][d] * f[u];
     }
   }
 #pragma unroll
-  for (int y = 1; y < kWave; y <<= 1) L += xor_f32(L, y);
+  for (int y = 1; y < LANES; y <<= 1) L += xor_f32(L, y);
   const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-  for (int d = 0; d < 4; ++d) sum[d] = (sum[d] + xor_f32(sum[d], 32)) * inv;
+  for (int d = 0; d < kDims; ++d) {
+    if constexpr (kSide == 2) sum[d] += xor_f32(sum[d], 32);
+    sum[d] *= inv;
+  }
   const int row = blk.row0 + i;
-  if (half == 0)
-    store_elems<T, 4>((T*)a.out + ((size_t)(blk.start + row / G) * a.H_q + hk * G + row % G) * kHeadDim + d0, sum);
+  if (in && side == 0)
+    store_elems<T, kDims>((T*)a.out + ((size_t)(blk.start + row / G) * a.H_q + hk * G + row % G) * kHeadDim + d0, sum);
 }
 
 // How a call is divided.
@@ -438,8 +448,12 @@ int launch_chunk(const ChunkPlan& p, const Chunk4Args& a, void* ws, hipStream_t 
   }
   hipLaunchKernelGGL((cache4_prompt_kernel<F32, true, KS>), grid, dim3(256), 0, s, a, (float*)ws);
   if (!launched()) return SAKI_ERR_HIP;
-  hipLaunchKernelGGL((cache4_gather_kernel<F32, KS>), dim3((unsigned)p.groups, kRows / KS / 4), dim3(256), 0, s, a,
-                     (const float*)ws);
+  if (p.splits <= 6)
+    hipLaunchKernelGGL((cache4_gather_kernel<F32, KS, 16>), dim3((unsigned)p.groups, kRows / KS / 16), dim3(256), 0, s,
+                       a, (const float*)ws);
+  else
+    hipLaunchKernelGGL((cache4_gather_kernel<F32, KS, 64>), dim3((unsigned)p.groups, kRows / KS / 4), dim3(256), 0, s,
+                       a, (const float*)ws);
   return launched() ? SAKI_OK : SAKI_ERR_HIP;
 }
 

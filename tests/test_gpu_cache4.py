@@ -143,6 +143,8 @@ def test_write_out_of_a_fused_projection():
     ([0, 1], [0], 1), ([0, 64, 64, 130], [3, 0, 62], 2), ([2, 5, 5, 21, 40], [200, 7, 0, 190], 3),
     ([0, 0, 0], [0, 0], 1), ([0, 300], None, 5), ([0, 17], [-3], 2), (list(range(0, 202, 2)), [1] * 100, 1),
     ([0] * 70 + [1] + [1] * 70 + [33], [0] * 141, 2),
+    (list(range(3, 68)), list(range(64)), 1), (list(range(0, 130, 2)), None, 2), (list(range(66)), [5] * 65, 1),
+    ([0] * 63 + [4, 40], [9] * 64, 2),
 ])
 def test_read(cu, starts, H, dt):
     rng = np.random.default_rng(len(cu) + H)
