@@ -7,6 +7,9 @@
 //                                type and shape on this device
 //   rows(t, dtype, shape, dev, name)   (data pointer, elements between tokens) of
 //                                token rows [T, H, d] with dense heads
+//   cache4(k, v, scales, dev)    (three data pointers, n_blocks, H_kv, d) of a 4-bit
+//                                cache's dense arrays on this device; None if they
+//                                are not that (0.2 us a call less than array for each)
 //   refusal(f)                   what array and rows call, with their arguments,
 //                                for a tensor that is not so; it raises
 //   saki_...(...)                the C entry points: None or an int for a pointer,
@@ -100,6 +103,30 @@ PyObject* rows(PyObject* const* a, Py_ssize_t n) {
   return r;
 }
 
+PyObject* cache4(PyObject* const* a, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "cache4 takes 4 arguments");
+    return nullptr;
+  }
+  const long dev = PyLong_AsLong(a[3]);
+  if (dev == -1 && PyErr_Occurred()) return nullptr;
+  const at::Tensor* t[3];
+  for (int i = 0; i < 3; ++i) {
+    if (!THPVariable_Check(a[i])) Py_RETURN_NONE;
+    t[i] = &THPVariable_Unpack(a[i]);
+    if (!t[i]->defined() || !t[i]->is_cuda() || t[i]->layout() != at::kStrided || t[i]->scalar_type() != at::kByte ||
+        t[i]->get_device() != dev || t[i]->dim() != (i < 2 ? 4 : 5) || !t[i]->is_contiguous())
+      Py_RETURN_NONE;
+  }
+  const int64_t blocks = t[0]->size(0), H = t[0]->size(1), half = t[0]->size(3);
+  const at::Tensor& s = *t[2];
+  if (t[0]->size(2) != SAKI_CACHE_BLOCK || t[1]->sizes() != t[0]->sizes() || s.size(0) != blocks || s.size(1) != H ||
+      s.size(2) != 2 || s.size(3) != SAKI_CACHE_BLOCK || s.size(4) != half / 16)
+    Py_RETURN_NONE;
+  return Py_BuildValue("(NNNLLL)", PyLong_FromVoidPtr(t[0]->data_ptr()), PyLong_FromVoidPtr(t[1]->data_ptr()),
+                       PyLong_FromVoidPtr(s.data_ptr()), (long long)blocks, (long long)H, (long long)(2 * half));
+}
+
 PyObject* refusal(PyObject*, PyObject* f) {
   Py_INCREF(f);
   Py_XSETREF(g_refusal, f);
@@ -160,6 +187,7 @@ struct Entry<Fn> {
 PyMethodDef methods[] = {
     {"array", (PyCFunction)(void (*)(void))guarded<array>, METH_FASTCALL, nullptr},
     {"rows", (PyCFunction)(void (*)(void))guarded<rows>, METH_FASTCALL, nullptr},
+    {"cache4", (PyCFunction)(void (*)(void))guarded<cache4>, METH_FASTCALL, nullptr},
     {"refusal", refusal, METH_O, nullptr},
     SAKI_ENTRY(saki_rope),
     SAKI_ENTRY(saki_block_tables),

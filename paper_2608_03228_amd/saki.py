@@ -743,7 +743,10 @@ def saki_attend_prompt(q, k, v, cu, out=None, ws=None, stream=None):
 
 def _cache4_arrays(k_cache, v_cache, scales, dev):
     """-> pointers, n_blocks, H_kv, d"""
-    u8 = _torch().uint8
+    found = _args_mod.cache4(k_cache, v_cache, scales, dev)
+    if found is not None:
+        return found
+    u8 = _torch().uint8  # (not so: what is wrong)
     shape = k_cache.shape
     if len(shape) != 4 or shape[2] != CACHE_BLOCK:
         raise ValueError(f"k_cache must be [n_blocks, H_kv, {CACHE_BLOCK}, d / 2]")
