@@ -17,6 +17,7 @@ import numpy as np
 import pytest
 
 import oracle as O
+from tests.test_gpu_streams import check_pools, made, zeros  # noqa: F401  (made: a fixture)
 
 torch = pytest.importorskip("torch")
 S = pytest.importorskip("paper_2608_03228_amd.saki")
@@ -630,6 +631,33 @@ def test_calls_on_a_stream_of_the_callers():
     got = S.saki_cache4_attend(*args, stream=stream), S.saki_cache4_prompt(*chunk, stream=stream)
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+@pytest.mark.parametrize("name", ["attend", "prompt"])
+def test_new_tensors_come_from_the_streams_memory(made, name):
+    """An output and a workspace (wide tables)."""
+    u8, i32 = dict(dtype=torch.uint8), dict(dtype=torch.int32)
+    cache = zeros(2, 2, 64, 64, **u8), zeros(2, 2, 64, 64, **u8), zeros(2, 2, 2, 64, 4, **u8)
+    tab, lens, cu = zeros(1, 100, **i32), zeros(1, **i32) + 70, torch.tensor([0, 9], device=DEV, **i32)
+    if name == "attend":
+        check_pools(made, lambda s: S.saki_cache4_attend(zeros(1, 4, 1, 128), *cache, tab, lens, stream=s), 2)
+    else:
+        check_pools(made, lambda s: S.saki_cache4_prompt(zeros(9, 4, 128), *cache, tab, lens, cu, stream=s), 2)
+
+
+def test_a_cache_of_no_block():
+    u8 = dict(dtype=torch.uint8, device=DEV)
+    cache = torch.empty(0, 2, 64, 64, **u8), torch.empty(0, 2, 64, 64, **u8), torch.empty(0, 2, 2, 64, 4, **u8)
+    x, tab, lens, cu = torch.ones(3, 2, 128, device=DEV), ints([[0, 5]]), ints([100]), ints([0, 3])
+    S.saki_cache4_write(x, x, ints([0, 1, 2]), *cache)
+    k, v = S.saki_cache4_read(*cache, tab, cu, x.clone(), x.clone())
+    assert (k == 0).all() and (v == 0).all()
+    q = torch.ones(1, 4, 1, 128, device=DEV)
+    assert (S.saki_cache4_attend(q, *cache, tab, lens) == 0).all()
+    assert (S.saki_cache4_attend(q, *cache, tab, lens, top_idx=ints(np.zeros((1, 4, 1, 2)))) == 0).all()
+    assert (S.saki_cache4_attend(q, *cache, ints(np.zeros((1, 100))), lens) == 0).all()
+    for t in (tab, ints(np.zeros((1, 400)))):
+        assert (S.saki_cache4_prompt(torch.ones(3, 4, 128, device=DEV), *cache, t, lens, cu) == 0).all()
 
 
 def test_offsets_past_32_bits():
