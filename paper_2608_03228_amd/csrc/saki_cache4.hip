@@ -317,7 +317,8 @@ __device__ __forceinline__ long long share4_at(long long tile, const Share& s) {
 // them in registers only while they are multiplied: with the next one on its way in
 // registers too a wave held 200 of them, and two groups a CU gave 79 us for
 // attend_batch_131k and 37.8 for attend_drafts_9k of the timed cases (here 75.9 and
-// 33.6).  Bound by HBM and by the conversions: 353 MB in 71 us, 5.0 TB/s (5.4 with the
+// 33.6; 89 and 39.7 with a tile's values still on their way while its keys are
+// multiplied, each wait then in the middle of the products).  Bound by HBM and by the conversions: 353 MB in 71 us, 5.0 TB/s (5.4 with the
 // loads alone); about 400 vector instructions a tile and wave, 0.9 us of a SIMD.
 // A short call is a chain of reads (lengths, table, tile) and one tile's products.
 //
@@ -544,7 +545,8 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 3) void cache4_attend_kernel(C
           sum += p[j];
         }
         l += sum;
-        const int turn = (n / 4 * 8 + 9) % 32;  // brings the group's byte of a token's scales to the exponent's place (the rest is ignored)
+        // brings the group's byte of a token's scales to the exponent's place (the rest is ignored)
+        const int turn = (n / 4 * 8 + 9) % 32;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {  // tokens 32 half + 4 g .. + 3 and + 16 .. + 19 of the lane
           bf16x8_t pt[kPT];

@@ -42,16 +42,17 @@ __device__ __forceinline__ float swap32(float v) { return xor_f32(v, 32); }
 // goes through the keys in the cache's blocks of 64: each thread holds 16 bytes of
 // the next block's keys and values, converts them to bf16 with their scales
 // (exactly) and puts them into LDS, two blocks deep, while the block before is
-// multiplied.  Two groups a CU fill each other's pauses.  S^T = K Q^T leaves a lane with scores of one row, so the softmax is
-// in registers but for one exchange, and its weights are at once the operand of
-// O^T = V^T P^T, whose other operand the transposing LDS reads form.  bf16: weights
-// rounded to bf16; float32: queries and weights in three bf16 terms, 32 keys at a
-// time for the registers' sake.
+// multiplied.  Two groups a CU fill each other's pauses.  S^T = K Q^T leaves a lane
+// with scores of one row, so the softmax is in registers but for one exchange, and
+// its weights are at once the operand of O^T = V^T P^T, whose other operand the
+// transposing LDS reads form.  bf16: weights rounded to bf16; float32: queries and
+// weights in three bf16 terms, 32 keys at a time for the registers' sake.
 //
 // Bound by power and the MFMA, with the softmax beside it: 2,000 tokens of 32 / 8
 // heads over 23,000 and 32,800 keys in 950-1,060 us, 0.88-0.98 PFLOP/s depending on
 // the card (a large bf16 matrix product reaches 1.17-1.27), the MFMA 41% busy;
-// float32, three products each, 0.36 PFLOP/s.  256 rows a work-group, which halves the conversions, took as long.
+// float32, three products each, 0.36 PFLOP/s.  256 rows a work-group, which halves
+// the conversions, took as long.
 //
 // KS = 2: 64 rows, and two waves share a row's keys, 32 of each block; their sums
 // meet at the end (see chunk_plan).
