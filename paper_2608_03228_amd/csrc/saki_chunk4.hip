@@ -356,7 +356,9 @@ __global__ __launch_bounds__(256) void cache4_gather_kernel(Chunk4Args a, const 
   for (int d = 0; d < kDims; ++d) sum[d] = 0.f;
   for (int s0 = 0; s0 < a.splits; s0 += LANES) {
     const int n = min(a.splits - s0, LANES);
-    float e = 0.f;  // a part's factor; 0: no key of it is seen (a NaN goes on)
+    // a part's factor; below 0: no key of it is seen, and its sums may never have been written.  A factor of zero
+    // is another matter (keys that score far below the others): its sums may be NaN, and the row is then, too
+    float e = -1.f;
     if (s0 + c < parts) {
       const float l = wl[(s0 + c) * kPart];
       if (l != 0.f) e = __builtin_amdgcn_exp2f((wm[(s0 + c) * kPart] - ref) * (kScale * kLog2e)), L += l * e;
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(256) void cache4_gather_kernel(Chunk4Args a, const 
         f[u] = __shfl(e, first + t % LANES);
 #pragma unroll
         for (int d = 0; d < kDims; ++d) z[u][d] = 0.f;
-        if (t < n && f[u] != 0.f) load_elems<float, kDims>(w + (s0 + t) * kPart + i * kHeadDim + d0, z[u]);
+        if (t < n && !(f[u] < 0.f)) load_elems<float, kDims>(w + (s0 + t) * kPart + i * kHeadDim + d0, z[u]);
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u)
