@@ -77,8 +77,9 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
   // this lane's row, its token, head and position; the least and largest position
   // of the group's rows and of the wave's
   const int row = min(rw + n, n_rows - 1) + blk.row0, tok = row / G;
-  // (a length near the lowest int stands for none, as others below zero do)
-  const int before = (int)max((long long)a.lens[blk.b] - blk.len, -(1LL << 30));
+  // the first row's position: a request's last token stands at lens - 1, also where its offsets end past the T
+  // tokens of the call.  (A length near the lowest int stands for none, as others below zero do.)
+  const int before = (int)max((long long)a.lens[blk.b] - a.cu[blk.b + 1] + blk.start, -(1LL << 30));
   const int pos = before + tok;
   const int pos_min = before + blk.row0 / G, pos_max = before + (blk.row0 + n_rows - 1) / G;
   const int pos_lo = before + (blk.row0 + min(rw, n_rows - 1)) / G;
