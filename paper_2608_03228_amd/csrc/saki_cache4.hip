@@ -442,10 +442,15 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 3) void cache4_attend_kernel(C
           load_elems<__bf16, 8>((const __bf16*)q + at, x);
       }
       bf16x8_t qf[kQT];
-      if constexpr (F32)
+      if constexpr (F32) {
         side_by_side<RP>(x, term, qf);
-      else
+      } else {
+        // an infinite element is taken as NaN, as the row is by the formula: the products may give one infinity
+        // for all its scores, which are a row without a key then (the terms of float32 are NaN by themselves)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], 0.f, x[e]);
         split_bf16<1>(x, qf);
+      }
 #pragma unroll
       for (int x = 0; x < kQT; ++x) __builtin_memcpy(&s_q[kQT * wave + x][lane], &qf[x], 16);
     }
@@ -779,6 +784,9 @@ __global__ __launch_bounds__(64) void cache4_lists_kernel(CacheArgs a, const voi
   const int c = lane % 4, e0 = lane / 4, m = lane % 16, g = lane / 16;
   float qx[32];
   load_elems<T, 32>((const T*)q + r * kHeadDim + 32 * c, qx);
+  float odd = 0.f;  // NaN where an element is not finite: the row is, also where all its scores are -infinity
+#pragma unroll
+  for (int e = 0; e < 32; ++e) odd = fmaf(qx[e], 0.f, odd);
   uint4 kx[4];
   uint32_t vx[16], se[2];  // se: the keys' scales of entries 32 u + lane (lanes 0 .. 31), the values' (32 .. 63)
 #pragma unroll
@@ -808,7 +816,7 @@ __global__ __launch_bounds__(64) void cache4_lists_kernel(CacheArgs a, const voi
   for (int u = 0; u < 4; ++u) {
     const uint32_t w[4] = {kx[u].x, kx[u].y, kx[u].z, kx[u].w};
     const float f = scale_of((uint32_t)__shfl((int)se[u / 2], 16 * (u % 2) + e0) >> (8 * c) & 255);
-    float s = 0.f;
+    float s = odd;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       float y[8];

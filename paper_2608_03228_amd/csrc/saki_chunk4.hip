@@ -240,6 +240,19 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
   // read by vector loads, 1.05 us for 0.88 a block of 64 rows)
   __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
   fetch(at1);
+  if constexpr (!F32) {
+    // a row with an infinite query is NaN, but products alone may give one infinity for all its scores, which are
+    // a row without a key then: one element NaN makes them NaN (the terms of float32 do so by themselves)
+    uint32_t odd = 0;  // the top bit of a half: an exponent of ones
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      uint32_t w[4];
+      __builtin_memcpy(w, &q[s][0], 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= (w[e] & 0x7f807f80u) + 0x00800080u;
+    }
+    if (odd & 0x80008000u) q[0][0][0] = (__bf16)NAN;
+  }
   auto step = [&](int t, const uint8_t* now, uint8_t* next) __attribute__((always_inline)) {
     __syncthreads();  // block t is in `now`, and `next` is read
     const int at3 = block_of(t + 3);
