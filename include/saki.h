@@ -513,6 +513,9 @@ int saki_attend_prompt(const void* q, const void* k, const void* v, int dtype, i
  *     values.
  *   - scales: device [n_blocks, H_kv, 2 (keys, values), 64 (tokens), 4 (groups)]
  *     bytes.  All three are 16-byte aligned; H_kv * n_blocks < 2^25.
+ *   - SAKI_ERR_UNSUPPORTED: d other than 128, a dtype other than float32 and bf16,
+ *     H_kv above 32,767, tables of more than 2^25 - 2 blocks a request, and what the
+ *     entry points name beside it.
  */
 
 /*
@@ -559,8 +562,10 @@ size_t saki_cache4_attend_workspace_bytes(int B, int H_q, int H_kv, int Q, int m
  * saki_cache4_attend (GPU) -- saki_cache_attend over the 4-bit cache: attention of
  * the Q newest tokens' queries per request and head, over every key that they see
  * or, with top_idx, over the listed ones.  The arguments are those of
- * saki_cache_attend.  Elements and their scales enter the products exactly.  A NaN
- * group makes the rows that see it NaN (a value's in its dims), and no others.
+ * saki_cache_attend.  At most 2^22 groups of 16 rows, B * H_kv * ceil(H_q / H_kv * Q
+ * / 16), and 2^25 rows B * H_q * Q.  Elements and their scales enter the products exactly.  A NaN
+ * group makes the rows that see it NaN (a value's in its dims), and no others; a
+ * query with an element that is not finite makes its row NaN if it sees a key.
  */
 int saki_cache4_attend(const void* q, int dtype, int B, int H_q, int H_kv, int Q, int d,
                        const void* k_cache, const void* v_cache, const void* scales, int n_blocks,
@@ -581,11 +586,14 @@ size_t saki_cache4_prompt_workspace_bytes(int dtype, int T, int B, int H_q, int 
  * conversation differ in lens alone.  A row without a key writes zeros.  bf16
  * queries meet the elements in exact products and weights are rounded to bf16 for
  * theirs; float32 queries and weights are taken as three bf16 terms (2^-25 of
- * them is left out).
+ * them is left out).  NaN groups and queries that are not finite as in
+ * saki_cache4_attend.  T <= 2^26, T * H_q / H_kv < 2^30 - 1, H_q <= 65,535 and
+ * (T * H_q / H_kv / 128 + B) * H_kv <= 2^22.
  *
  *   q       device [T, H_q, d] rows ld_q apart
  *   tables  device int [B, max_blocks];  lens  device int [B], the new tokens counted
- *   cu      device int [B + 1], ascending
+ *   cu      device int [B + 1], ascending, 0 and more; where it ends above T, only the
+ *           first T tokens are here, at the positions that they have in the whole
  *   out     device [T, H_q, d], dense, overlaps no input; tokens of no request are
  *           left as they were
  *   ws      device workspace of saki_cache4_prompt_workspace_bytes(...), 16-byte
