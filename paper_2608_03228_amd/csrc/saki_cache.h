@@ -138,7 +138,6 @@ __device__ __forceinline__ int tiles_of(int len, int max_blocks) {
 constexpr int kPartRows = 16;
 constexpr int kPartFloats = kPartRows * kHeadDim + 2 * kPartRows;  // sums, maxima, weights
 constexpr int kMinPiece = 4;                                       // tiles a work-group takes at least
-constexpr int kAttendGroups = 512;                                 // two a CU
 
 // Tiles of up to 64 requests, one a lane: its own, the sum up to it, and all
 // (below 2^31, as a table has fewer than 2^25 - 1 blocks).
@@ -166,13 +165,6 @@ __device__ __forceinline__ Sums wave_sums(const CacheArgs& a) {
 struct Share {
   long long total, piece;
 };
-__device__ __forceinline__ Share share_of(long long total, int groups) {
-  Share s;
-  s.total = total;
-  s.piece = (total + groups - 1) / groups;
-  if (s.piece < kMinPiece) s.piece = kMinPiece;
-  return s;
-}
 
 // ---------------------------------------------------------------- argument checks
 

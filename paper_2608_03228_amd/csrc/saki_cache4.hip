@@ -17,8 +17,9 @@ namespace {
 // a token and 8 dims a lane; four lanes hold a group and find its largest element.
 // Four tokens whose slots stand together fill 256 contiguous bytes of codes, in
 // either layout.  Groups have their own scales, so that nothing there before is
-// read.  HBM bound on prompts: 30,400 float32 tokens of 4 heads in 31 us, 4.6 TB/s;
-// bf16 in 17.1 (20.3 with four tokens a wave and their loads behind the slots').
+// read.  HBM bound on prompts: 39,000 float32 tokens of 4 heads (187 MB) in 36 us,
+// 5.2 TB/s; bf16 in 21 (a fifth more with four tokens a wave and their loads behind
+// the slots').
 constexpr int kWriteTokens = 8;  // of a wave
 template <typename T>
 __global__ __launch_bounds__(256) void cache4_write_kernel(const T* __restrict__ k, const T* __restrict__ v,
@@ -61,7 +62,11 @@ __global__ __launch_bounds__(256) void cache4_write_kernel(const T* __restrict__
 
 // ---------------------------------------------------------------- reading back
 
-constexpr size_t kL2Bytes = 32u << 20;  // of the eight dies
+// The eight dies' L2s: outputs of that size and more are stored past them.  us, bf16 of
+// 8 heads, stores that stay / that do not: 16 MB 6.7 / 6.3, 32 MB 10.0 / 8.4, 64 MB
+// 15.9 / 13.4, 128 MB 28.7 / 28.8, 256 MB 66.9 / 53.6; float32 6.5 / 6.3, 9.4 / 7.8,
+// 14.8 / 15.0, 26.1 / 27.1, 67.9 / 55.6.
+constexpr size_t kL2Bytes = 32u << 20;
 
 struct Read4Args {
   const uint8_t *k, *v, *scales;
@@ -81,8 +86,8 @@ struct Read4Args {
 // output a lane.
 //
 // Bound by its stores: a wave's fill whole lines, and past what the L2s hold (NT)
-// they do not stay there: 470 MB in 98 us, 4.8 TB/s (137 with stores that stay, 176
-// with 32 bytes a lane); 310 MB as bf16 in 58 (78).
+// they do not stay there: 472 MB (nine tenths written) in 70 us, 6.7 TB/s (106 with
+// stores that stay); 361 MB as bf16 in 55 (75).
 template <typename T>
 constexpr int read_rows() {
   return 4 * kWave / (kHeadDim * (int)sizeof(T) / 16);
@@ -283,8 +288,8 @@ __device__ __forceinline__ void hide_values(uint4* e, int g, int whole, int some
   }
 }
 
-// share_of, in 32 bits where they do (a division in 64 takes 0.2 us of a step's 13),
-// and with shares of 8 tiles at least where pairs have more than 256: of one pair's
+// As many tiles for each group, divided in 32 bits where they do (in 64 it takes 0.2 us
+// of a step's 13), 4 at least, and 8 at least where pairs have more than 256: of one pair's
 // 1,563 tiles 391 parts take longer to join (21.0 us in all) than 196 (15.6); of
 // 141 tiles it is 10.3 us for 36 parts and 11.2 for 18.
 __device__ __forceinline__ Share share4_of(long long total, int groups, long long pairs) {
@@ -315,12 +320,15 @@ __device__ __forceinline__ long long share4_at(long long tile, const Share& s) {
 //
 // Each wave brings its tiles (8.7 KB) to LDS by direct loads, one at a time, and has
 // them in registers only while they are multiplied: with the next one on its way in
-// registers too a wave held 200 of them, and two groups a CU gave 79 us for
-// attend_batch_131k and 37.8 for attend_drafts_9k of the timed cases (here 75.9 and
-// 33.6; 89 and 39.7 with a tile's values still on their way while its keys are
-// multiplied, each wait then in the middle of the products).  Bound by HBM and by the conversions: 353 MB in 71 us, 5.0 TB/s (5.4 with the
-// loads alone); about 400 vector instructions a tile and wave, 0.9 us of a SIMD.
-// A short call is a chain of reads (lengths, table, tile) and one tile's products.
+// registers too a wave held 200 of them, and two groups a CU gave 79 us for 8 requests
+// of up to 131,072 keys (float32, 28 / 4 heads) and 37.8 for 16 of up to 9,000 and four
+// queries (bf16, 32 / 8), where this gives 75.9 and 33.6; 89 and 39.7 with a tile's
+// values still on their way while its keys are multiplied, each wait then in the
+// middle of the products.  (Both with the join.)  Bound by HBM and by the conversions:
+// the 353 MB of the first in 73-74 us, 4.8 TB/s (its loads alone reach 5.4), 706 MB of
+// bf16 and 32 / 8 heads in 132 with the join, 5.3; about 400 vector instructions a tile
+// and wave, 0.9 us of a SIMD.  A short call is a chain of reads (lengths, table, tile)
+// and one tile's products.
 //
 // Tried: products of the fp4 codes themselves with queries in E4M3 terms (16x16x128,
 // scales in the operands) save a sixth of the instructions and 1% of the time, but
@@ -889,6 +897,10 @@ void launch_attend4(int R, dim3 grid, hipStream_t s, const CacheArgs& a, const v
     hipLaunchKernelGGL((cache4_attend_kernel<F32, SPLIT, 16, W>), grid, dim3(64 * W), 0, s, a, q, out, ws);
 }
 
+// Eight waves a pair for less than 64 pairs.  us in all (bf16, 32 / 8 heads, lengths of
+// a quarter to the whole of the width), eight waves / four: 8 pairs of 600 tiles 18.0 /
+// 18.9, 32 24.6 / 24.9, 64 40.9 / 40.2; of 200 tiles 12.2 / 12.6, 16.7 / 16.9, 23.5 /
+// 22.9, 128 pairs 31.8 / 30.3, 256 56.0 / 53.2.
 template <bool F32>
 void launch_join4(unsigned pairs, hipStream_t s, const CacheArgs& a, int groups, const float* ws, void* out) {
   const dim3 grid(pairs, pairs > 256 ? 1 : kHeadDim / 16);
@@ -913,8 +925,11 @@ void launch_join4(unsigned pairs, hipStream_t s, const CacheArgs& a, int groups,
 // 1024        16.3 / 23.4 / 35.8   22.8 / 31.5 / 44.8   40.7 / 47.6 / 62.3
 // float32, 28 / 4 heads: 4 pairs of 16 and 24 tiles 9.4 / 8.9 / 9.9 and 12.4 / 11.3 /
 // 10.3; 32 of 32 and 48 16.3 / 14.5 / 14.7 and 21.7 / 19.0 / 15.0; 256 of 48 23.8 /
-// 21.6 / 28.2.  (Many pairs: up to the width where one long request among short
-// ones would keep its groups at work alone for long.)
+// 21.6 / 28.2.  512 pairs of 96 tiles 49.8 / 48.4 / 55.5, 1,024 of 64 and 96 76.2 /
+// 76.0 / 84.9 and 114 / 108 / 118: many pairs would gain further still, but one long
+// request among short ones keeps its groups at work alone (512 pairs, one request of
+// 48, 64 and 96 tiles and the others of 5: 18.1 / 23.0, 22.7 / 23.1 and 32.5 / 26.5
+// with four waves and split).
 bool whole4_better(long long pairs, int max_blocks) {
   return max_blocks <= (pairs >= 512 ? 96 : pairs >= 128 ? 64 : pairs >= 64 ? 48 : pairs >= 16 ? 32 : 20);
 }
@@ -925,7 +940,8 @@ bool eight4_better(long long pairs, int max_blocks) {
 template <typename T>
 int launch_read4(const Read4Args& a, hipStream_t s) {
   const int sides = a.k_out && a.v_out ? 2 : 1;
-  // some 2,000 work-groups while the heads allow it
+  // some 2,000 work-groups while the heads allow it (us for 512, 1,024, 2,048 and 4,096 of them: 2,000 bf16 tokens
+  // of 32 heads 11.2, 10.3, 10.0, 10.0; 8,000 of 8 10.5, 9.9, 9.8, 9.8; few tokens alike)
   const int blocks = (a.T + read_rows<T>() - 1) / read_rows<T>(), most = (sides * a.H + 3) / 4;
   int split = 2048 / blocks;
   split = split < 1 ? 1 : split > most ? most : split;

@@ -45,13 +45,16 @@ __device__ __forceinline__ float swap32(float v) { return xor_f32(v, 32); }
 // multiplied.  Two groups a CU fill each other's pauses.  S^T = K Q^T leaves a lane
 // with scores of one row, so the softmax is in registers but for one exchange, and
 // its weights are at once the operand of O^T = V^T P^T, whose other operand the
-// transposing LDS reads form.  bf16: weights rounded to bf16; float32: queries and
-// weights in three bf16 terms, 32 keys at a time for the registers' sake.
+// transposing LDS reads form.  bf16: weights rounded to bf16, which takes a row's error
+// from 0.0016 of it (its output's rounding) to 0.0018-0.0019; a second term would be as
+// many products again as the values take now.  float32: queries and weights in three
+// bf16 terms, 32 keys at a time for the registers' sake.
 //
 // Bound by power and the MFMA, with the softmax beside it: 2,000 tokens of 32 / 8
 // heads over 23,000 and 32,800 keys in 950-1,060 us, 0.88-0.98 PFLOP/s depending on
-// the card (a large bf16 matrix product reaches 1.17-1.27), the MFMA 41% busy;
-// float32, three products each, 0.36 PFLOP/s.  256 rows a work-group, which halves
+// the card (a large bf16 matrix product reaches 1.17-1.27), the MFMA 41% busy, and a
+// whole prompt of 8,192 in 605, 0.91; float32, three products each, 0.36 PFLOP/s (the
+// prompt 0.39).  256 rows a work-group, which halves
 // the conversions, took as long.
 //
 // KS = 2: 64 rows, and two waves share a row's keys, 32 of each block; their sums

@@ -403,6 +403,16 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const T* __restrict__ 
 
 // ---------------------------------------------------------------- attention over the cache
 
+constexpr int kAttendGroups = 512;  // two a CU
+
+__device__ __forceinline__ Share share_of(long long total, int groups) {
+  Share s;
+  s.total = total;
+  s.piece = (total + groups - 1) / groups;
+  if (s.piece < kMinPiece) s.piece = kMinPiece;
+  return s;
+}
+
 // Eight E4M3 codes as bf16 (exact: a code has at most 4 significant bits).
 __device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi) {
   uint32_t w[4];
