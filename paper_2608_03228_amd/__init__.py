@@ -3,7 +3,8 @@
 The compute lives in libsaki.so (host float64 calibration + gfx950 HIP
 kernels, C ABI in include/saki.h): the index, and serving around it (rotary
 positions, block tables, paged caches in 8 and 4 bits, their attention and that
-of whole prompts).  ``paper_2608_03228_amd.saki`` is its thin ctypes binding.  Build with ``python -m paper_2608_03228_amd.build``.
+of whole prompts).  ``paper_2608_03228_amd.saki`` is its thin ctypes binding.
+Build with ``python -m paper_2608_03228_amd.build``.
 """
 from . import saki  # noqa: F401
 from .saki import (  # noqa: F401

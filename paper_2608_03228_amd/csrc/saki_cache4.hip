@@ -41,7 +41,8 @@ __global__ __launch_bounds__(256) void cache4_write_kernel(const T* __restrict__
     if (slot[u] >= n_blocks * kTile) slot[u] = -1;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
-    if (t < (uint32_t)n_tokens) load_elems<T, 8>((which ? v + t * ld_v : k + t * ld_k) + (size_t)h * kHeadDim + 8 * m, x[u]);
+    if (t < (uint32_t)n_tokens)
+      load_elems<T, 8>((which ? v + t * ld_v : k + t * ld_k) + (size_t)h * kHeadDim + 8 * m, x[u]);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -98,7 +99,8 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(Read4Args a) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int t0 = blockIdx.x * kReadRows, t = t0 + lane % kReadRows;
   auto at = [&](int b) { return min(max(a.cu[b], 0), a.T); };
-  int mine = 0, first, begin, end, start;  // this row's request: its first row and the one behind its last, its first token
+  // this row's request: its first row and the one behind its last, its first token
+  int mine = 0, first, begin, end, start;
   if (a.B <= kWave) {  // all offsets and starts in a wave's lanes, one read deep
     const int c = at(min(lane, a.B)), last = at(a.B), s = a.starts && lane < a.B ? a.starts[lane] : 0;
 #pragma unroll
@@ -145,7 +147,8 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(Read4Args a) {
   const uint64_t rows = __ballot(row);
   if (!rows) return;
   // a lane stores 16 bytes: kDims elements of one row
-  constexpr int kDims = 16 / sizeof(T), kLanes = kHeadDim / kDims, kAtOnce = kWave / kLanes, kLoads = kReadRows / kAtOnce;
+  constexpr int kDims = 16 / sizeof(T), kLanes = kHeadDim / kDims, kAtOnce = kWave / kLanes;
+  constexpr int kLoads = kReadRows / kAtOnce;
   const int c = lane % kLanes, m = c * kDims / 8, q = lane / kLanes;
   int blks[kLoads], tokens[kLoads];
 #pragma unroll
@@ -421,7 +424,8 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 3) void cache4_attend_kernel(C
     };
     // (block, head)'s bytes to LDS: each lane's 16 where it reads them again
     auto stage = [&](int blk, uint8_t* to) __attribute__((always_inline)) {
-      const size_t at = (size_t)blk * a.H_kv + hk;  // (the same in all lanes: addresses are a scalar and 32 bits a lane)
+      // (the same in all lanes: addresses are a scalar and 32 bits a lane)
+      const size_t at = (size_t)blk * a.H_kv + hk;
       const uint8_t *kp = a.k + at * kCodes4, *vp = a.v + at * kCodes4, *sp = (const uint8_t*)a.scales + at * kScales4;
       const uint32_t k_off = n * 64 + g * 16, v_off = lane * 16, s_off = lane * 4;
 #pragma unroll

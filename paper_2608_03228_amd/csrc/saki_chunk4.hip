@@ -131,7 +131,8 @@ __global__ __launch_bounds__(256, 2) void cache4_prompt_kernel(Chunk4Args a, flo
     for (int s = 0; s < 4; ++s) {
       uint32_t w[4];
       decode8(kc[s], scale_of(ks), w);
-      *reinterpret_cast<uint4*>(to + r * 256 + (((tid % 4 * 4 + s) ^ (r % 16)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(to + r * 256 + (((tid % 4 * 4 + s) ^ (r % 16)) * 16)) =
+          make_uint4(w[0], w[1], w[2], w[3]);
     }
     float f[4];  // (the conversion reads the exponent alone)
 #pragma unroll
@@ -445,7 +446,8 @@ ChunkPlan chunk_plan(int dtype, int T, int B, int G, int H_kv, int max_blocks) {
     const long long n = blocks_of(rows, block_rows, B) * H_kv;
     const long long shares[4] = {1, 256 / n, 512 / n, 1024 / n};
     for (int i = 0; i < 4; ++i) {
-      const long long most = max_blocks < 4 ? 1 : max_blocks / 2, s = shares[i] < most ? shares[i] : most;  // two blocks each at least
+      const long long most = max_blocks < 4 ? 1 : max_blocks / 2;  // two blocks each at least
+      const long long s = shares[i] < most ? shares[i] : most;
       if (i && s <= 1) continue;
       const long long all = n * s, rest = all % 512;
       const float each = (float)((max_blocks + s - 1) / s);
