@@ -543,7 +543,8 @@ int saki_cache4_write(const void* k, const void* v, int dtype, int T, int H_kv, 
  * ctx_lens as starts) or whole contexts (starts NULL: from token 0).
  *
  *   tables  device int [B, max_blocks]
- *   starts  device int [B], or NULL;  cu  device int [B + 1], ascending
+ *   starts  device int [B], or NULL;  cu  device int [B + 1], ascending, 0 and more;
+ *           rows from T on are left out
  *   k_out, v_out  device [T, H_kv, d], rows ld_k, ld_v apart; either may be NULL
  * A token without a block in its table reads as zeros; rows of no request are
  * left as they were.  T <= 2^26.  The outputs overlap neither each other nor an
